@@ -362,6 +362,80 @@ fibattn_status_t fibattn_rope_qk_table(const void *q, const void *k, void *q_out
                                        const float *theta, float *alpha, const int32_t *base, int K,
                                        int W, void *table, fibattn_dtype_t dtype, hipStream_t stream);
 
+/*
+ * Dense attention to states that are not the sequence's own: an encoder's states of
+ * another length S, or rows that the whole batch shares (a memory, a prompt).
+ *   query t of (b, h) reads every row j < len of its key/value head:
+ *   o = sum_j softmax_j(tau <q, k_j>) v_j, lse the natural-log log-sum-exp, tau =
+ *   1/sqrt(d_head).
+ *   q, o : [B, H, T, d_head]; k, v : [B_kv, H_kv, S, d_head], H_kv dividing H and B_kv =
+ *          B, or 1: one set of states for the batch, read once for all its queries
+ *   lens : device int32 [B_kv], valid rows of each entry (clamped to [0, S]; rows behind
+ *          them are not read), or NULL: S.  Without a row (len 0) o is 0 and lse -inf.
+ *   layouts : placements of q, k, v, o (element strides, multiples of 16 bytes; rows of
+ *          d_head elements contiguous and 16-byte aligned), or NULL: packed
+ *   workspace : fibattn_cross_workspace_bytes(...) bytes of device memory, 16-byte aligned
+ *          (0 bytes: none needed; also for sizes that the call refuses).  Calls that
+ *          overlap in time, graph replays among them, need a workspace each.
+ * Inputs and outputs must not overlap.  Limits: d_head in {32, 64, 128}; B*H <= 65535;
+ * B*H*T <= 2^30; S <= 2^30; rows of a head less than 2^22 elements apart: else
+ * FIBATTN_ERR_UNSUPPORTED.
+ */
+size_t fibattn_cross_workspace_bytes(int B, int B_kv, int H, int H_kv, int T, int S, int d_head);
+fibattn_status_t fibattn_cross_forward(const void *q, const void *k, const void *v, void *o, float *lse,
+                                       const int32_t *lens, void *workspace, size_t workspace_bytes,
+                                       const fibattn_layout_t *layouts, int B, int B_kv, int H,
+                                       int H_kv, int T, int S, int d_head, fibattn_dtype_t dtype,
+                                       hipStream_t stream);
+
+/*
+ * Its gradients: dq like q; dk, dv like k, summed over the query heads and, with B_kv = 1,
+ * over the batch (0 behind the lengths).  The weights are exp(tau <q, k_j> - lse) and the
+ * rows' <dO, o> is taken from o: lse and o may be those of a softmax over more than these
+ * states (fibattn_join); the gradients are then this part's share of it.
+ * layouts: q, k, v, o, dO, dq, dk, dv, or NULL: packed.  workspace:
+ * fibattn_cross_backward_workspace_bytes(...) bytes, never 0 for sizes in the limits.
+ */
+size_t fibattn_cross_backward_workspace_bytes(int B, int B_kv, int H, int H_kv, int T, int S, int d_head);
+fibattn_status_t fibattn_cross_backward(const void *q, const void *k, const void *v, const void *o,
+                                        const float *lse, const void *dO, void *dq, void *dk, void *dv,
+                                        const int32_t *lens, void *workspace, size_t workspace_bytes,
+                                        const fibattn_layout_t *layouts, int B, int B_kv, int H,
+                                        int H_kv, int T, int S, int d_head, fibattn_dtype_t dtype,
+                                        hipStream_t stream);
+
+/*
+ * Attention of a batch that shares a long prefix, in one softmax over the prefix and each
+ * sequence's own rows.  The prefix is read once for the batch.
+ *   q, o : [B, H, T, d_head], the newest T tokens of every sequence
+ *   k_prefix, v_prefix : [1, H_kv, P, d_head], read by every query
+ *   k, v : [B, H_kv, S, d_head], a sequence's own rows, the newest T of its lens[b] valid
+ *          ones (NULL: S) those of the queries: query t reads rows j <= lens[b] - T + t
+ *          (none where that is negative)
+ *   layouts: q, k_prefix, v_prefix, k, v, o, or NULL: packed; the batch stride of
+ *          k_prefix and v_prefix is not used.
+ * workspace: fibattn_prefix_workspace_bytes(...) bytes, never 0 for sizes in the limits of
+ * fibattn_cross_forward (P as S).
+ */
+size_t fibattn_prefix_workspace_bytes(int B, int H, int H_kv, int T, int P, int S, int d_head);
+fibattn_status_t fibattn_prefix_forward(const void *q, const void *k_prefix, const void *v_prefix,
+                                        const void *k, const void *v, void *o, float *lse,
+                                        const int32_t *lens, void *workspace, size_t workspace_bytes,
+                                        const fibattn_layout_t *layouts, int B, int H, int H_kv, int T,
+                                        int P, int S, int d_head, fibattn_dtype_t dtype,
+                                        hipStream_t stream);
+
+/*
+ * The attention over the union of two disjoint sets of keys from the attention over each
+ * (of fibattn_forward and fibattn_cross_forward, say): lse = log(exp(lse_a) + exp(lse_b)),
+ * o = exp(lse_a - lse) o_a + exp(lse_b - lse) o_b.  A part whose lse is -inf counts nothing
+ * whatever its o holds; with both so, o is 0 and lse -inf.  o and lse may be o_a and lse_a,
+ * or o_b and lse_b.  layouts: o_a, o_b, o, or NULL: packed [B, H, T, d_head].
+ */
+fibattn_status_t fibattn_join(const void *o_a, const float *lse_a, const void *o_b, const float *lse_b,
+                              void *o, float *lse, const fibattn_layout_t *layouts, int B, int H, int T,
+                              int d_head, fibattn_dtype_t dtype, hipStream_t stream);
+
 /* Human-readable name of a status code (static storage). */
 const char *fibattn_status_string(fibattn_status_t status);
 
@@ -372,7 +446,8 @@ const char *fibattn_status_string(fibattn_status_t status);
  * pair that takes the dispatch's
  * own start and end timestamps on the launch stream (0 rope, 1 forward, 2 backward
  * dq+dalpha, 3 backward dk/dv, which also sums dalpha, 4 unused: no launch has it, 5
- * device-alpha kernels).
+ * device-alpha kernels, 6 the forward of attention to other states, 7 its dq, 8 its dk/dv,
+ * 9 the joins and sums of partial results).
  * fibattn_timing_end(&avg_ms, &count) synchronises on the last event, returns
  * the mean launch duration and the number of launches timed, and stops timing.
  */

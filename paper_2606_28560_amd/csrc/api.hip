@@ -8,7 +8,7 @@
 #include <mutex>
 #include <vector>
 
-#include "../../include/fibattn.h"
+#include "checks.h"
 #include "launch.h"
 
 using namespace fibattn;
@@ -36,8 +36,6 @@ fibattn_status_t build_table(float alpha, const int32_t *base, int K, int W, Run
     return rung_table_fill(alpha, b, W, rt) ? FIBATTN_OK : FIBATTN_ERR_INVALID_ARG;
 }
 
-bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
-
 fibattn_status_t check_common(int B, int H, int T, int d_head, int W, int K, fibattn_dtype_t dtype) {
     if (B < 1 || H < 1 || T < 1 || W < 0 || K < 0) return FIBATTN_ERR_INVALID_ARG;
     if (dtype != FIBATTN_FP32 && dtype != FIBATTN_BF16) return FIBATTN_ERR_INVALID_ARG;
@@ -53,8 +51,6 @@ fibattn_status_t check_common(int B, int H, int T, int d_head, int W, int K, fib
     return FIBATTN_OK;
 }
 
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
 // Every tensor packed [B, heads, T, d].
 Layouts packed_layouts(int H, int H_kv, int T, int D) {
     const Layout lq = Layout::packed(H, T, D), lk = Layout::packed(H_kv, T, D);
@@ -67,8 +63,7 @@ Layouts packed_layouts(int H, int H_kv, int T, int D) {
 fibattn_status_t check_layout(const fibattn_layout_t &l, int T, int d_head, fibattn_dtype_t dtype,
                               Layout *out) {
     const long long es = dtype == FIBATTN_BF16 ? 2 : 4;
-    if (l.batch < 0 || l.head < 0 || l.pos < 0) return FIBATTN_ERR_INVALID_ARG;
-    if ((l.batch * es) % 16 || (l.head * es) % 16 || (l.pos * es) % 16) return FIBATTN_ERR_INVALID_ARG;
+    if (!strides_ok(l, dtype)) return FIBATTN_ERR_INVALID_ARG;
     if (((long long)(T - 1) * l.pos + d_head) * es >= (1ll << 31)) return FIBATTN_ERR_UNSUPPORTED;
     *out = {l.batch, l.head, l.pos};
     return FIBATTN_OK;

@@ -1,0 +1,510 @@
+// Dense attention of queries to states of another length, and the join of partial results.
+//
+//   s_rj = tau <q_r, k_j>,  o_r = sum_j exp(s_rj - lse_r) v_j,  lse_r = log sum_j exp(s_rj)
+// in one pass over j with the running maximum and sum of each row, in float32.
+#include "cross_launch.h"
+
+namespace fibattn {
+
+namespace {
+
+// Rows of the states a workgroup stages at a time when its waves share them.
+template <typename S> constexpr int kStage = sizeof(S) == 2 ? 64 : 32;
+
+template <typename S, int D> constexpr int lds_bytes() {
+    // shared: K and V, two stages; per wave: K and V of 32 rows
+    constexpr int shared = 2 * 2 * kStage<S> * D * (int)sizeof(S), waves = 4 * 2 * 32 * D * (int)sizeof(S);
+    constexpr int merge = 4 * 32 * D * 4;
+    return shared > waves ? (shared > merge ? shared : merge) : (waves > merge ? waves : merge);
+}
+
+// A wave's 32 query rows.
+template <typename S, int D> struct Rows {
+    Frag<S> q[D / 16];
+    f32x16_t acc[D / 32];  // transposed: column = row of the lane
+    float m, l;            // running maximum (in powers of two) and the lane's own part of the sum
+    int lim;               // rows of the states that this row reads
+    long long id;          // (b H + h) T + t
+    RowAt at;
+    bool on;
+};
+
+template <typename S, int D>
+__device__ __forceinline__ void load_rows(const Queries &a, const States &st, int b0, int j, int r0, int len,
+                                          Rows<S, D> &w) {
+    const int lane = threadIdx.x & 63, h = lane >> 5, r = r0 + (lane & 31);
+    w.on = r < st.rows;
+    w.at = row_at(a, b0, j, min(r, st.rows - 1));
+    w.id = ((long long)w.at.b * a.H + w.at.h) * a.T + w.at.t;
+    w.lim = st.causal ? min(len - a.T + 1 + w.at.t, len) : len;
+    const S *row = (const S *)a.q + w.at.b * a.lq.sb + w.at.h * a.lq.sh + w.at.t * a.lq.st;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) load_frag(row, ks, h, w.q[ks]);
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) w.acc[dt] = zero16();
+    w.m = -INFINITY;
+    w.l = 0.f;
+}
+
+template <typename S, int D>
+__device__ __forceinline__ f32x16_t logits(const char *kt, int row0, const Rows<S, D> &w) {
+    const int lane = threadIdx.x & 63;
+    f32x16_t s = zero16();
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        Frag<S> f;
+        Tile<S, D>::row_frag(kt, row0 + (lane & 31), ks, lane >> 5, f);
+        s = mma(f, w.q[ks], s);
+    }
+    return s;
+}
+
+// Rows of the states from `base` that a query does not read count nothing.
+template <typename S, int D>
+__device__ __forceinline__ void mask(f32x16_t &s, int base, const Rows<S, D> &w) {
+    const int h = (threadIdx.x >> 5) & 1;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (base + 8 * (i >> 2) + 4 * h + (i & 3) >= w.lim) s[i] = -INFINITY;
+}
+
+// Logits to weights exp2(s - m).  The reference m moves only when a logit passes it by 8
+// powers of two: the sums keep their 24 bits and the accumulators are rarely rescaled.
+template <typename S, int D, int N>
+__device__ __forceinline__ void weights(f32x16_t *s, float scale, Rows<S, D> &w) {
+    float top = s[0][0];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+    top = half_max(top) * scale;
+    if (__ballot(top > w.m + 8.f)) {
+        const float m = fmaxf(top, w.m);
+        const float f = m == -INFINITY ? 1.f : ex2(w.m - m);
+        w.m = m;
+        w.l *= f;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) w.acc[dt] *= f;
+    }
+    const float m = w.m == -INFINITY ? 0.f : w.m;
+    float l = 0.f;
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[n][i] = ex2(fmaf(s[n][i], scale, -m));
+            l += s[n][i];
+        }
+    w.l += l;
+}
+
+template <typename S, int D>
+__device__ __forceinline__ void values(const char *vt, int row0, const f32x16_t &p, Rows<S, D> &w) {
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        Frag<S> pf;
+        to_frag(p, a, pf);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) {
+            Frag<S> f;
+            Tile<S, D>::operand_t(vt, row0 + 16 * a, dt, f);
+            w.acc[dt] = mma(f, pf, w.acc[dt]);
+        }
+    }
+}
+
+// o and lse of a row (or its partial results), from the sum l over both halves.
+__device__ __forceinline__ void put_lse(const Queries &a, long long slot, long long id, float m, float l) {
+    const float z = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
+    if (a.part_lse)
+        a.part_lse[slot * a.B * a.H * a.T + id] = z;
+    else
+        a.lse[id] = z;
+}
+
+template <typename S, int D>
+__device__ __forceinline__ S *out_row(const Queries &a, const RowAt &at) {
+    return (S *)a.o + at.b * a.lo.sb + at.h * a.lo.sh + at.t * a.lo.st;
+}
+
+// One problem's rows of the states; stage i holds rows i NT .. of k, then of v.
+template <typename S, int D> struct Source {
+    const char *k, *v;
+    long long ks, vs;
+    int len;
+    __device__ __forceinline__ void fetch(char *dst, int i, int wv) const {
+        constexpr int NT = kStage<S>;
+        const int r = i * NT;
+        Tile<S, D>::template stage<NT, 4>(dst, k + r * ks, ks, len - r, wv);
+        Tile<S, D>::template stage<NT, 4>(dst + NT * Tile<S, D>::kRow, v + r * vs, vs, len - r, wv);
+    }
+};
+
+// Fetches the next stage and works on the present one.  `restrict`: the loads into the next
+// stage's LDS are not waited for by the reads of this one's.
+template <typename S, int D>
+__device__ __forceinline__ void rows_step(const char *__restrict cur, char *__restrict next, const Source<S, D> &src,
+                                          int i, bool more, int wv, int low, bool idle, float scale, Rows<S, D> &w) {
+    constexpr int NT = kStage<S>, NS = NT / 32, TB = NT * Tile<S, D>::kRow;
+    if (more) src.fetch(next, i + 1, wv);
+    if (idle) return;
+    f32x16_t s[NS];
+#pragma unroll
+    for (int e = 0; e < NS; ++e) s[e] = logits<S, D>(cur, 32 * e, w);
+    if ((i + 1) * NT > low) {
+#pragma unroll
+        for (int e = 0; e < NS; ++e) mask<S, D>(s[e], i * NT + 32 * e, w);
+    }
+    weights<S, D, NS>(s, scale, w);
+#pragma unroll
+    for (int e = 0; e < NS; ++e) values<S, D>(cur + TB, 32 * e, s[e], w);
+}
+
+// 128 query rows, 32 to a wave; the waves share the staged rows of the states.
+template <typename S, int D>
+__device__ __forceinline__ void rows_body(const Queries &a, const States &st, int item, char *lds) {
+    typedef Tile<S, D> X;
+    constexpr int NT = kStage<S>, TB = NT * X::kRow;
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = item % st.tiles, piece = item / st.tiles % st.splits, prob = item / st.tiles / st.splits;
+    const int b0 = prob / a.Hkv, j = prob % a.Hkv;
+    const int len = states_len(st, b0);
+    Rows<S, D> w;
+    load_rows<S, D>(a, st, b0, j, 128 * tile + 32 * wv, len, w);
+    const bool idle = 128 * tile + 32 * wv >= st.rows;
+
+    const int n = (len + NT - 1) / NT;
+    const int n0 = (int)((long long)n * piece / st.splits), n1 = (int)((long long)n * (piece + 1) / st.splits);
+    const int low = st.causal ? max(len - a.T + 1, 0) : len;  // rows that every query reads
+    const char *kp = (const char *)((const S *)st.k + b0 * st.lk.sb + j * st.lk.sh);
+    const char *vp = (const char *)((const S *)st.v + b0 * st.lv.sb + j * st.lv.sh);
+    const long long ks = st.lk.st * (long long)sizeof(S), vs = st.lv.st * (long long)sizeof(S);
+    const Source<S, D> src = {kp, vp, ks, vs, len};
+    if (n0 < n1) src.fetch(lds, n0, wv);
+    for (int i = n0; i < n1; ++i) {
+        wait_loads<0>();
+        __syncthreads();  // this stage has arrived, the one before has been read
+        const int buf = (i - n0) & 1;
+        rows_step<S, D>(lds + buf * 2 * TB, lds + (buf ^ 1) * 2 * TB, src, i, i + 1 < n1, wv, low, idle, a.scale, w);
+    }
+    const float l = half_sum(w.l), f = l == 0.f ? 0.f : 1.f / l;
+    if (!w.on) return;
+    const long long slot = st.slot + piece;
+    if (lane < 32) put_lse(a, slot, w.id, w.m, l);
+    if (a.part_o)
+        store_cols<D>(a.part_o + (slot * a.B * a.H * a.T + w.id) * D, w.acc, f, lane >> 5);
+    else
+        store_cols<D>(out_row<S, D>(a, w.at), w.acc, f, lane >> 5);
+}
+
+// 32 query rows for all four waves, each on its own rows of the states (tiles of 32, one in
+// four), staged for the wave alone; joined in LDS.
+template <typename S, int D>
+__device__ __forceinline__ void keys_body(const Queries &a, const States &st, int item, char *lds) {
+    typedef Tile<S, D> X;
+    constexpr int TB = 32 * X::kRow, OPS = 32 / X::kRowsPerLoad;
+    __shared__ float stat[2][4][32];
+    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
+    const int tile = item % st.tiles, piece = item / st.tiles % st.splits, prob = item / st.tiles / st.splits;
+    const int b0 = prob / a.Hkv, j = prob % a.Hkv;
+    const int len = states_len(st, b0);
+    Rows<S, D> w;
+    load_rows<S, D>(a, st, b0, j, 32 * tile, len, w);
+    const int n = (len + 31) / 32;
+    const int n0 = (int)((long long)n * piece / st.splits), n1 = (int)((long long)n * (piece + 1) / st.splits);
+    const int low = st.causal ? max(len - a.T + 1, 0) : len;
+    const char *kp = (const char *)((const S *)st.k + b0 * st.lk.sb + j * st.lk.sh);
+    const char *vp = (const char *)((const S *)st.v + b0 * st.lv.sb + j * st.lv.sh);
+    const long long ks = st.lk.st * (long long)sizeof(S), vs = st.lv.st * (long long)sizeof(S);
+    char *kt = lds + 2 * TB * wv, *vt = kt + TB;
+    int i = n0 + wv;
+    if (i < n1) {
+        X::template stage<32, 1>(kt, kp + 32 * i * ks, ks, len - 32 * i, 0);
+        X::template stage<32, 1>(vt, vp + 32 * i * vs, vs, len - 32 * i, 0);
+    }
+    for (; i < n1; i += 4) {
+        const bool more = i + 4 < n1;
+        wait_loads<OPS>();  // K is here, V may be on its way
+        f32x16_t s = logits<S, D>(kt, 0, w);
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // K has been read
+        if (more) X::template stage<32, 1>(kt, kp + 32 * (i + 4) * ks, ks, len - 32 * (i + 4), 0);
+        if (32 * (i + 1) > low) mask<S, D>(s, 32 * i, w);
+        weights<S, D, 1>(&s, a.scale, w);
+        if (more)
+            wait_loads<OPS>();
+        else
+            wait_loads<0>();
+        values<S, D>(vt, 0, s, w);
+        __builtin_amdgcn_s_waitcnt(0xC07F);  // V has been read
+        if (more) X::template stage<32, 1>(vt, vp + 32 * (i + 4) * vs, vs, len - 32 * (i + 4), 0);
+    }
+    // the waves' results of each row, in the order of the waves
+    const float l = half_sum(w.l);
+    __syncthreads();
+    float *part = (float *)lds;
+    store_cols<D>(part + (32 * wv + (lane & 31)) * D, w.acc, 1.f, h);
+    if (h == 0) {
+        stat[0][wv][lane] = w.m;
+        stat[1][wv][lane] = l;
+    }
+    __syncthreads();
+    const long long slot = st.slot + piece;
+    constexpr int V = 4, per = D / V;  // lanes to a row
+    for (int e = threadIdx.x; e < 32 * per; e += 256) {
+        const int r = e / per, d = e % per * V;
+        if (32 * tile + r >= st.rows) continue;
+        float m = stat[0][0][r];
+#pragma unroll
+        for (int x = 1; x < 4; ++x) m = fmaxf(m, stat[0][x][r]);
+        float sum = 0.f;
+        f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+            // a wave that met no rows has the maximum -inf: it counts nothing
+            const float f = stat[0][x][r] == -INFINITY ? 0.f : ex2(stat[0][x][r] - m);
+            sum += stat[1][x][r] * f;
+            y += *reinterpret_cast<const f32x4_t *>(part + (32 * x + r) * D + d) * f;
+        }
+        const float f = sum == 0.f ? 0.f : 1.f / sum;
+        const RowAt at = row_at(a, b0, j, 32 * tile + r);
+        const long long id = ((long long)at.b * a.H + at.h) * a.T + at.t;
+        if (d == 0) put_lse(a, slot, id, m, sum);
+        if (a.part_o) {
+            *reinterpret_cast<f32x4_t *>(a.part_o + (slot * a.B * a.H * a.T + id) * D + d) = y * f;
+        } else {
+            S *row = out_row<S, D>(a, at) + d;
+            if constexpr (sizeof(S) == 4)
+                *reinterpret_cast<f32x4_t *>(row) = y * f;
+            else
+                *reinterpret_cast<uint2 *>(row) = make_uint2(pack2(y[0] * f, y[1] * f), pack2(y[2] * f, y[3] * f));
+        }
+    }
+}
+
+// Whether rows of the states that only some queries read hold an infinity or NaN among their
+// values: a weight of 0 times such a value would reach the queries that do not read it.
+template <typename S, int D>
+__device__ __forceinline__ bool not_finite(const Queries &a, const States &st, int item) {
+    const int prob = item / st.tiles / st.splits, b0 = prob / a.Hkv, j = prob % a.Hkv;
+    const int len = states_len(st, b0), low = max(len - a.T + 1, 0);
+    const S *v = (const S *)st.v + b0 * st.lv.sb + j * st.lv.sh;
+    constexpr int N = 16 / (int)sizeof(S), per = D / N;
+    int bad = 0;
+    for (int e = threadIdx.x; e < (len - low) * per; e += 256) {
+        float x[N];
+        Vec<S>::load(v + (low + e / per) * st.lv.st + e % per * N, x);
+#pragma unroll
+        for (int i = 0; i < N; ++i) bad |= !(fabsf(x[i]) < INFINITY);
+    }
+    return __syncthreads_or(bad);
+}
+
+__device__ __forceinline__ float value_of(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ float value_of(float x) { return x; }
+__device__ __forceinline__ void put_value(uint16_t *p, float x) { *p = (uint16_t)f32_to_bf16(x); }
+__device__ __forceinline__ void put_value(float *p, float x) { *p = x; }
+
+// A wave per query row, one row of the states at a time, and only those the query reads.
+// For causal states with values that are not finite (not_finite).
+template <typename S, int D>
+__device__ __forceinline__ void plain_body(const Queries &a, const States &st, int item, int tile_rows) {
+    constexpr int N = (D + 63) / 64;
+    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+    const int tile = item % st.tiles, piece = item / st.tiles % st.splits, prob = item / st.tiles / st.splits;
+    const int b0 = prob / a.Hkv, j = prob % a.Hkv;
+    const int len = states_len(st, b0);
+    const S *k = (const S *)st.k + b0 * st.lk.sb + j * st.lk.sh, *v = (const S *)st.v + b0 * st.lv.sb + j * st.lv.sh;
+    const int n0 = (int)((long long)len * piece / st.splits), n1 = (int)((long long)len * (piece + 1) / st.splits);
+    const long long slot = st.slot + piece;
+    for (int r = tile * tile_rows + wv; r < min((tile + 1) * tile_rows, st.rows); r += 4) {
+        const RowAt at = row_at(a, b0, j, r);
+        const long long id = ((long long)at.b * a.H + at.h) * a.T + at.t;
+        const S *q = (const S *)a.q + at.b * a.lq.sb + at.h * a.lq.sh + at.t * a.lq.st;
+        const int lim = min(st.causal ? len - a.T + 1 + at.t : len, n1);
+        float x[N], y[N], m = -INFINITY, l = 0.f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            x[n] = lane + 64 * n < D ? value_of(q[lane + 64 * n]) : 0.f;
+            y[n] = 0.f;
+        }
+        for (int c = n0; c < lim; ++c) {
+            float s = 0.f;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+                if (lane + 64 * n < D) s = fmaf(x[n], value_of(k[c * st.lk.st + lane + 64 * n]), s);
+#pragma unroll
+            for (int e = 32; e; e >>= 1) s += __shfl_xor(s, e, 64);
+            s *= a.scale;
+            const float top = fmaxf(m, s), f = top == -INFINITY ? 1.f : ex2(m - top);
+            const float p = ex2(s - (top == -INFINITY ? 0.f : top));
+            m = top;
+            l = fmaf(l, f, p);
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+                if (lane + 64 * n < D) y[n] = fmaf(p, value_of(v[c * st.lv.st + lane + 64 * n]), y[n] * f);
+        }
+        const float f = l == 0.f ? 0.f : 1.f / l;
+        if (lane == 0) put_lse(a, slot, id, m, l);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            if (lane + 64 * n < D) {
+                if (a.part_o)
+                    a.part_o[(slot * a.B * a.H * a.T + id) * D + lane + 64 * n] = y[n] * f;
+                else
+                    put_value(out_row<S, D>(a, at) + lane + 64 * n, y[n] * f);
+            }
+    }
+}
+
+// Items of the first states, then of the second (a prefix, then the sequence's own rows).
+template <typename S, int D>
+__global__ __launch_bounds__(256, 2) void cross_fwd_kernel(Queries a, States s0, States s1, int by_keys0, int by_keys1,
+                                                           int n0, int n) {
+    __shared__ __attribute__((aligned(16))) char lds[lds_bytes<S, D>()];
+    const int b = blockIdx.y * gridDim.x + blockIdx.x;
+    if (b >= n) return;
+    const bool first = b < n0;
+    const States st = first ? s0 : s1;
+    const int item = first ? xcd_item(b, n0) : xcd_item(b - n0, n - n0);
+    const bool by_keys = first ? by_keys0 : by_keys1;
+    if (st.causal && not_finite<S, D>(a, st, item))
+        plain_body<S, D>(a, st, item, by_keys ? 32 : 128);
+    else if (by_keys)
+        keys_body<S, D>(a, st, item, lds);
+    else
+        rows_body<S, D>(a, st, item, lds);
+}
+
+// Partial results of a row: o = sum_i exp(lse_i - lse) o_i, lse = log sum_i exp(lse_i).  A
+// part without rows (lse -inf) counts nothing, whatever its o holds.
+template <typename S, int D>
+__global__ __launch_bounds__(256) void join_parts_kernel(Queries a, int parts) {
+    constexpr int per = D / 4;
+    const long long rows = (long long)a.B * a.H * a.T;
+    const long long e = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
+    const long long r = e / per;
+    const int d = (int)(e % per) * 4;
+    if (r >= rows) return;
+    float m = -INFINITY;
+    for (int i = 0; i < parts; ++i) m = fmaxf(m, a.part_lse[i * rows + r]);
+    float sum = 0.f;
+    f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < parts; ++i) {
+        const float z = a.part_lse[i * rows + r];
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(a.part_o + (i * rows + r) * D + d);
+        if (z == -INFINITY) continue;
+        const float f = ex2((z - m) * kLog2e);
+        sum += f;
+        y += x * f;
+    }
+    const float f = sum == 0.f ? 0.f : 1.f / sum;
+    const int t = (int)(r % a.T), h = (int)(r / a.T % a.H), b = (int)(r / a.T / a.H);
+    if (d == 0) a.lse[r] = sum == 0.f ? -INFINITY : m + __log2f(sum) * kLn2;
+    S *row = out_row<S, D>(a, {b, h, t}) + d;
+    if constexpr (sizeof(S) == 4)
+        *reinterpret_cast<f32x4_t *>(row) = y * f;
+    else
+        *reinterpret_cast<uint2 *>(row) = make_uint2(pack2(y[0] * f, y[1] * f), pack2(y[2] * f, y[3] * f));
+}
+
+// The same for two stored results over disjoint sets of keys.
+template <typename S, int D>
+__global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
+    constexpr int N = 16 / (int)sizeof(S), per = D / N;
+    const long long rows = (long long)a.B * a.H * a.T;
+    const long long e = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
+    const long long r = e / per;
+    const int d = (int)(e % per) * N;
+    if (r >= rows) return;
+    const int t = (int)(r % a.T), h = (int)(r / a.T % a.H), b = (int)(r / a.T / a.H);
+    const float za = a.za[r], zb = a.zb[r];
+    const float m = fmaxf(za, zb);
+    const float fa = za == -INFINITY ? 0.f : ex2((za - m) * kLog2e), fb = zb == -INFINITY ? 0.f : ex2((zb - m) * kLog2e);
+    const float sum = fa + fb, f = sum == 0.f ? 0.f : 1.f / sum;
+    float x[N], y[N], o[N];
+    Vec<S>::load((const S *)a.a + b * a.la.sb + h * a.la.sh + t * a.la.st + d, x);
+    Vec<S>::load((const S *)a.b + b * a.lb.sb + h * a.lb.sh + t * a.lb.st + d, y);
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = (fa == 0.f ? 0.f : x[i] * fa * f) + (fb == 0.f ? 0.f : y[i] * fb * f);
+    Vec<S>::store((S *)a.o + b * a.lo.sb + h * a.lo.sh + t * a.lo.st + d, o);
+    if (d == 0) a.z[r] = sum == 0.f ? -INFINITY : m + __log2f(sum) * kLn2;
+}
+
+// Row tiles and pieces of states for `prob` problems.  Few rows (at most 32 to a problem) go
+// to workgroups whose waves take different rows of the states.
+void plan(States *s, int prob, int *by_keys) {
+    *by_keys = s->rows <= 32;
+    s->tiles = (s->rows + (*by_keys ? 31 : 127)) / (*by_keys ? 32 : 128);
+    const long long wgs = (long long)prob * s->tiles;
+    // two workgroups to a CU; a piece keeps 256 rows or more
+    const long long want = (512 + wgs - 1) / wgs, most = (s->S + 255) / 256;
+    s->splits = (int)(want < 1 ? 1 : want < most ? want : most);
+    if (s->splits > 64) s->splits = 64;
+}
+
+template <typename S, int D>
+hipError_t forward(const Queries &a, States s0, const States *s1, int prob0, int prob1, hipStream_t st) {
+    int k0, k1 = 0;
+    plan(&s0, prob0, &k0);
+    States second = s0;
+    long long n0 = (long long)prob0 * s0.tiles * s0.splits, n = n0;
+    int parts = s0.splits;
+    s0.slot = 0;
+    if (s1) {
+        second = *s1;
+        plan(&second, prob1, &k1);
+        second.slot = parts;
+        parts += second.splits;
+        n += (long long)prob1 * second.tiles * second.splits;
+    }
+    if (n >= 1ll << 31) return hipErrorInvalidValue;
+    Queries q = a;
+    if (parts == 1) q.part_o = q.part_lse = nullptr;
+    hipError_t e = launch(kCrossForward, cross_fwd_kernel<S, D>, grid_of(n), dim3(256), 0, st, q, s0, second, k0, k1,
+                          (int)n0, (int)n);
+    if (e != hipSuccess || parts == 1) return e;
+    const long long threads = (long long)a.B * a.H * a.T * (D / 4);
+    return launch(kJoin, join_parts_kernel<S, D>, grid_of((threads + 255) / 256), dim3(256), 0, st, q, parts);
+}
+
+template <typename S>
+hipError_t forward_d(int D, const Queries &a, const States &s0, const States *s1, int prob0, int prob1, hipStream_t st) {
+    switch (D) {
+        case 32: return forward<S, 32>(a, s0, s1, prob0, prob1, st);
+        case 64: return forward<S, 64>(a, s0, s1, prob0, prob1, st);
+        default: return forward<S, 128>(a, s0, s1, prob0, prob1, st);
+    }
+}
+
+template <typename S> hipError_t join_d(int D, const JoinArgs &a, hipStream_t st) {
+    const long long rows = (long long)a.B * a.H * a.T, per = D * (long long)sizeof(S) / 16;
+    const dim3 grid = grid_of((rows * per + 255) / 256);
+    switch (D) {
+        case 32: return launch(kJoin, join_kernel<S, 32>, grid, dim3(256), 0, st, a);
+        case 64: return launch(kJoin, join_kernel<S, 64>, grid, dim3(256), 0, st, a);
+        default: return launch(kJoin, join_kernel<S, 128>, grid, dim3(256), 0, st, a);
+    }
+}
+
+}  // namespace
+
+int cross_forward_parts(int rows, int S, int prob) {
+    States s{};
+    s.rows = rows;
+    s.S = S;
+    int k;
+    plan(&s, prob, &k);
+    return s.splits;
+}
+
+hipError_t launch_cross_forward(int dtype, int D, const Queries &a, const States &s0, const States *s1, int prob0,
+                                int prob1, hipStream_t s) {
+    return dtype == 1 ? forward_d<uint16_t>(D, a, s0, s1, prob0, prob1, s)
+                      : forward_d<float>(D, a, s0, s1, prob0, prob1, s);
+}
+
+hipError_t launch_join(int dtype, int D, const JoinArgs &a, hipStream_t s) {
+    return dtype == 1 ? join_d<uint16_t>(D, a, s) : join_d<float>(D, a, s);
+}
+
+}  // namespace fibattn

@@ -10,7 +10,10 @@
 namespace fibattn {
 
 // 4: the dalpha sum, which the dk/dv launch carries
-enum KernelId { kRope = 0, kForward = 1, kBwdDq = 2, kBwdDkDv = 3, kAlpha = 5, kNumKernels = 6 };
+enum KernelId {
+    kRope = 0, kForward = 1, kBwdDq = 2, kBwdDkDv = 3, kAlpha = 5,
+    kCrossForward = 6, kCrossBwdDq = 7, kCrossBwdDkDv = 8, kJoin = 9, kNumKernels = 10
+};
 
 // The start/stop event pair for the next launch of kernel `id` while kernel timing is
 // active for it; false otherwise.

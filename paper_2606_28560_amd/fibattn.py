@@ -21,7 +21,8 @@ FIBATTN_FP32, FIBATTN_BF16 = 0, 1
 MAX_RUNGS = 32
 MAX_WINDOW = 128
 # "dalpha_reduce" names no launch: the dk/dv launch sums dalpha
-KERNEL_IDS = {"rope": 0, "forward": 1, "bwd_dq": 2, "bwd_dkdv": 3, "dalpha_reduce": 4, "alpha": 5}
+KERNEL_IDS = {"rope": 0, "forward": 1, "bwd_dq": 2, "bwd_dkdv": 3, "dalpha_reduce": 4, "alpha": 5,
+              "cross_forward": 6, "cross_bwd_dq": 7, "cross_bwd_dkdv": 8, "join": 9}
 EXPORTED = ("fibattn_rung_table", "fibattn_forward", "fibattn_backward_workspace_bytes",
             "fibattn_backward", "fibattn_forward_gqa", "fibattn_backward_gqa",
             "fibattn_forward_strided", "fibattn_backward_strided",
@@ -29,7 +30,9 @@ EXPORTED = ("fibattn_rung_table", "fibattn_forward", "fibattn_backward_workspace
             "fibattn_backward_dt", "fibattn_alpha_from_theta", "fibattn_dtheta", "fibattn_rope",
             "fibattn_rope_qk", "fibattn_status_string", "fibattn_timing_begin", "fibattn_timing_end",
             "fibattn_backward_noalloc", "fibattn_device_table_theta", "fibattn_rope_qk_table",
-            "fibattn_forward_rope_q", "fibattn_forward_rope_q_dt", "fibattn_forward_rope_q_strided")
+            "fibattn_forward_rope_q", "fibattn_forward_rope_q_dt", "fibattn_forward_rope_q_strided",
+            "fibattn_cross_workspace_bytes", "fibattn_cross_forward", "fibattn_cross_backward_workspace_bytes",
+            "fibattn_cross_backward", "fibattn_prefix_workspace_bytes", "fibattn_prefix_forward", "fibattn_join")
 SCRATCH_BYTES = 64 << 20  # FIBATTN_SCRATCH_BYTES: the allocation-free backward's static scratch
 
 
@@ -103,6 +106,20 @@ def lib():
     L.fibattn_backward_noalloc.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                            i, i, i, i, i, i, ip, i, f, f, i, vp]
     L.fibattn_backward_noalloc.restype = i
+    L.fibattn_cross_workspace_bytes.argtypes = [i] * 7
+    L.fibattn_cross_workspace_bytes.restype = sz
+    L.fibattn_cross_forward.argtypes = [vp] * 7 + [sz, vp] + [i] * 8 + [vp]
+    L.fibattn_cross_forward.restype = i
+    L.fibattn_cross_backward_workspace_bytes.argtypes = [i] * 7
+    L.fibattn_cross_backward_workspace_bytes.restype = sz
+    L.fibattn_cross_backward.argtypes = [vp] * 11 + [sz, vp] + [i] * 8 + [vp]
+    L.fibattn_cross_backward.restype = i
+    L.fibattn_prefix_workspace_bytes.argtypes = [i] * 7
+    L.fibattn_prefix_workspace_bytes.restype = sz
+    L.fibattn_prefix_forward.argtypes = [vp] * 9 + [sz, vp] + [i] * 8 + [vp]
+    L.fibattn_prefix_forward.restype = i
+    L.fibattn_join.argtypes = [vp] * 7 + [i] * 5 + [vp]
+    L.fibattn_join.restype = i
     L.fibattn_status_string.argtypes = [i]
     L.fibattn_status_string.restype = ctypes.c_char_p
     L.fibattn_timing_begin.argtypes = [i, i]
@@ -574,6 +591,227 @@ def fibattn_rope_qk_table(q, k, rope_base: float = 10000.0, *, theta=None, base=
                                      _stream(stream))
     _check("fibattn_rope_qk_table", st)
     return q_out, k_out, table
+
+
+# ---- attention to states that are not the sequence's own ----------------------------
+
+def _rows(name, t, shape, like):
+    """t: [.., .., .., D] of `shape` with contiguous rows, of like's dtype and device."""
+    if t.shape != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != like.dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {like.dtype}")
+    if t.device != like.device:
+        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    if t.stride(3) != 1:
+        raise ValueError(f"{name} must have contiguous rows (last-dimension stride 1)")
+
+
+def _vector(name, t, shape, dtype, like):
+    """t: a contiguous tensor of `shape` and dtype on like's device."""
+    if t.shape != shape or t.dtype != dtype or t.device != like.device or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on {like.device}")
+
+
+def _places(*ts):
+    """Placements of the tensors (None where all are packed); a dimension of one element
+    has no stride of its own."""
+    if _packed(*ts):
+        return None
+    arr = (ctypes.c_int64 * (3 * len(ts)))()
+    for a, t in enumerate(ts):
+        for d in range(3):
+            arr[3 * a + d] = t.stride(d) if t.shape[d] > 1 else 0
+    return arr
+
+
+def _heads_of(q, k, B_kv):
+    if k.dim() != 4 or k.shape[3] != q.shape[3] or k.shape[1] < 1 or q.shape[1] % k.shape[1] or k.shape[0] not in B_kv:
+        raise ValueError(f"k: shape {tuple(k.shape)} does not group q {tuple(q.shape)}")
+    return q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3]
+
+
+def _at(t, stream):
+    """A context that makes t's device, and `stream` if given, current for the allocations
+    and launches of a call (None: they are so already)."""
+    import torch
+
+    if t.dim() != 4 or not t.is_cuda:
+        raise ValueError("queries must be a GPU tensor [B,H,T,D]")
+    if stream is not None:
+        if stream.device != t.device:
+            raise ValueError(f"stream is on {stream.device}, expected {t.device}")
+        return torch.cuda.stream(stream)
+    if t.get_device() != torch.cuda.current_device():
+        return torch.cuda.device(t.device)
+    return None
+
+
+def _scratch(need, workspace, like):
+    """A workspace of `need` bytes: the caller's, or a new one."""
+    if workspace is None:
+        import torch
+
+        return torch.empty(need, device=like.device, dtype=torch.uint8) if need else None
+    if workspace.device != like.device or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {like.device}")
+    return workspace
+
+
+def _bytes(workspace):
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+
+
+def fibattn_cross_workspace_bytes(B: int, B_kv: int, H: int, H_kv: int, T: int, S: int, d_head: int) -> int:
+    return int(lib().fibattn_cross_workspace_bytes(B, B_kv, H, H_kv, T, S, d_head))
+
+
+def fibattn_cross_forward(q, k, v, lens=None, *, o=None, lse=None, workspace=None, stream=None):
+    """o, lse = dense attention of q [B,H,T,D] to states k, v [B_kv,H_kv,S,D] of another
+    length: H_kv divides H, and B_kv is B, or 1 for states that the whole batch shares.
+
+    lens: int32 device tensor [B_kv] of valid rows (clamped to 0..S; rows behind them are
+    not read), or None.  A sequence without a row gets o = 0, lse = -inf.  q, k, v, o may be
+    views with contiguous 16-byte aligned rows; lse is packed float32 [B,H,T]."""
+    ctx = _at(q, stream)
+    if ctx is not None:
+        with ctx:
+            return fibattn_cross_forward(q, k, v, lens, o=o, lse=lse, workspace=workspace)
+    import torch
+
+    B, H, Hkv, T, S, D = _heads_of(q, k, (q.shape[0], 1))
+    dtype = _dtype_code(q)
+    if o is None:
+        o = torch.empty_like(q, memory_format=torch.contiguous_format)
+    for n_, t, sh in (("q", q, q.shape), ("k", k, k.shape), ("v", v, k.shape), ("o", o, q.shape)):
+        _rows(n_, t, sh, q)
+    if lse is None:
+        lse = torch.empty((B, H, T), device=q.device, dtype=torch.float32)
+    else:
+        _vector("lse", lse, (B, H, T), torch.float32, q)
+    if lens is not None:
+        _vector("lens", lens, (k.shape[0],), torch.int32, q)
+    L = lib()
+    sizes = (B, k.shape[0], H, Hkv, T, S, D)
+    workspace = _scratch(L.fibattn_cross_workspace_bytes(*sizes), workspace, q)
+    st = L.fibattn_cross_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+                                 None if lens is None else lens.data_ptr(), *_bytes(workspace),
+                                 _places(q, k, v, o), *sizes, dtype, _stream(None))
+    _check("fibattn_cross_forward", st)
+    return o, lse
+
+
+def fibattn_cross_backward_workspace_bytes(B: int, B_kv: int, H: int, H_kv: int, T: int, S: int, d_head: int) -> int:
+    return int(lib().fibattn_cross_backward_workspace_bytes(B, B_kv, H, H_kv, T, S, d_head))
+
+
+def fibattn_cross_backward(q, k, v, o, lse, dO, lens=None, *, dq=None, dk=None, dv=None, workspace=None, stream=None):
+    """dq, dk, dv of fibattn_cross_forward; dk, dv sum over the query heads of a group and,
+    for states that the batch shares, over the batch, and are 0 behind the lengths.
+
+    o and lse may be those of a softmax over more keys than these (fibattn_join): the
+    gradients are then this part's share.  Every [..,D] tensor may be a view with contiguous
+    16-byte aligned rows; new outputs are packed."""
+    ctx = _at(q, stream)
+    if ctx is not None:
+        with ctx:
+            return fibattn_cross_backward(q, k, v, o, lse, dO, lens, dq=dq, dk=dk, dv=dv, workspace=workspace)
+    import torch
+
+    B, H, Hkv, T, S, D = _heads_of(q, k, (q.shape[0], 1))
+    dtype = _dtype_code(q)
+    packed = torch.contiguous_format
+    dq = torch.empty_like(q, memory_format=packed) if dq is None else dq
+    dk = torch.empty_like(k, memory_format=packed) if dk is None else dk
+    dv = torch.empty_like(k, memory_format=packed) if dv is None else dv
+    for n_, t, sh in (("q", q, q.shape), ("k", k, k.shape), ("v", v, k.shape), ("o", o, q.shape), ("dO", dO, q.shape),
+                      ("dq", dq, q.shape), ("dk", dk, k.shape), ("dv", dv, k.shape)):
+        _rows(n_, t, sh, q)
+    _vector("lse", lse, (B, H, T), torch.float32, q)
+    if lens is not None:
+        _vector("lens", lens, (k.shape[0],), torch.int32, q)
+    L = lib()
+    sizes = (B, k.shape[0], H, Hkv, T, S, D)
+    workspace = _scratch(L.fibattn_cross_backward_workspace_bytes(*sizes), workspace, q)
+    st = L.fibattn_cross_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+                                  dO.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                  None if lens is None else lens.data_ptr(), *_bytes(workspace),
+                                  _places(q, k, v, o, dO, dq, dk, dv), *sizes, dtype, _stream(None))
+    _check("fibattn_cross_backward", st)
+    return dq, dk, dv
+
+
+def fibattn_prefix_workspace_bytes(B: int, H: int, H_kv: int, T: int, P: int, S: int, d_head: int) -> int:
+    return int(lib().fibattn_prefix_workspace_bytes(B, H, H_kv, T, P, S, d_head))
+
+
+def fibattn_prefix_forward(q, k_prefix, v_prefix, k, v, lens=None, *, o=None, lse=None, workspace=None, stream=None):
+    """o, lse = attention of the newest T tokens of every sequence, q [B,H,T,D], to a prefix
+    stored once for the batch, k_prefix, v_prefix [1,H_kv,P,D], and to the sequence's own
+    rows k, v [B,H_kv,S,D], in one softmax.
+
+    lens: int32 device tensor [B] of valid own rows, the T new ones included (None: S);
+    query t reads the own rows j <= lens[b] - T + t.  q, the four states and o may be views
+    with contiguous 16-byte aligned rows."""
+    ctx = _at(q, stream)
+    if ctx is not None:
+        with ctx:
+            return fibattn_prefix_forward(q, k_prefix, v_prefix, k, v, lens, o=o, lse=lse, workspace=workspace)
+    import torch
+
+    B, H, Hkv, T, S, D = _heads_of(q, k, (q.shape[0],))
+    if k_prefix.dim() != 4 or k_prefix.shape[0] != 1 or k_prefix.shape[1] != Hkv or k_prefix.shape[3] != D:
+        raise ValueError(f"k_prefix has shape {tuple(k_prefix.shape)}, expected (1, {Hkv}, P, {D})")
+    P = k_prefix.shape[2]
+    dtype = _dtype_code(q)
+    if o is None:
+        o = torch.empty_like(q, memory_format=torch.contiguous_format)
+    for n_, t, sh in (("q", q, q.shape), ("k_prefix", k_prefix, k_prefix.shape),
+                      ("v_prefix", v_prefix, k_prefix.shape), ("k", k, k.shape), ("v", v, k.shape), ("o", o, q.shape)):
+        _rows(n_, t, sh, q)
+    if lse is None:
+        lse = torch.empty((B, H, T), device=q.device, dtype=torch.float32)
+    else:
+        _vector("lse", lse, (B, H, T), torch.float32, q)
+    if lens is not None:
+        _vector("lens", lens, (B,), torch.int32, q)
+    L = lib()
+    sizes = (B, H, Hkv, T, P, S, D)
+    workspace = _scratch(L.fibattn_prefix_workspace_bytes(*sizes), workspace, q)
+    st = L.fibattn_prefix_forward(q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                  o.data_ptr(), lse.data_ptr(), None if lens is None else lens.data_ptr(),
+                                  *_bytes(workspace), _places(q, k_prefix, v_prefix, k, v, o), *sizes, dtype,
+                                  _stream(None))
+    _check("fibattn_prefix_forward", st)
+    return o, lse
+
+
+def fibattn_join(o_a, lse_a, o_b, lse_b, *, o=None, lse=None, stream=None):
+    """o, lse over the union of two disjoint sets of keys from the attention over each, e.g.
+    of fibattn_forward (a sequence's own rows) and fibattn_cross_forward (shared ones).  A
+    part whose lse is -inf counts nothing.  o and lse may be o_a and lse_a or o_b and lse_b.
+
+    The backward of each part with the joined o and lse gives that part's gradients: dq is
+    the sum of the parts' dq (dalpha alone is not defined by one part's rows)."""
+    ctx = _at(o_a, stream)
+    if ctx is not None:
+        with ctx:
+            return fibattn_join(o_a, lse_a, o_b, lse_b, o=o, lse=lse)
+    import torch
+
+    B, H, T, D = o_a.shape
+    dtype = _dtype_code(o_a)
+    if o is None:
+        o = torch.empty_like(o_a, memory_format=torch.contiguous_format)
+    for n_, t in (("o_a", o_a), ("o_b", o_b), ("o", o)):
+        _rows(n_, t, o_a.shape, o_a)
+    lse = torch.empty((B, H, T), device=o_a.device, dtype=torch.float32) if lse is None else lse
+    for n_, t in (("lse_a", lse_a), ("lse_b", lse_b), ("lse", lse)):
+        _vector(n_, t, (B, H, T), torch.float32, o_a)
+    st = lib().fibattn_join(o_a.data_ptr(), lse_a.data_ptr(), o_b.data_ptr(), lse_b.data_ptr(), o.data_ptr(),
+                            lse.data_ptr(), _places(o_a, o_b, o), B, H, T, D, dtype, _stream(None))
+    _check("fibattn_join", st)
+    return o, lse
 
 
 def fibattn_timing_begin(kernel: str, capacity: int):

@@ -1,0 +1,361 @@
+"""Attention to other states on the GPU against 64 bits: the forward and the gradients over
+types, head layouts, lengths and placements; a prefix shared by the batch; the join with the
+sparse self-attention."""
+import math
+
+import pytest
+import torch
+
+from paper_2606_28560_amd import fibattn as F
+from paper_2606_28560_amd import schedules
+from tests import cross_reference as R
+
+pytestmark = pytest.mark.gpu
+
+BF, FP = torch.bfloat16, torch.float32
+
+
+def _normal(seed, *shape, dtype=FP):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda").to(dtype)
+
+
+def _inputs(dtype, B, Bk, H, Hkv, T, S, D, seed=0):
+    q, dO = _normal(seed, B, H, T, D, dtype=dtype), _normal(seed + 1, B, H, T, D, dtype=dtype)
+    k, v = (_normal(seed + n, Bk, Hkv, S, D, dtype=dtype) for n in (2, 3))
+    return q, k, v, dO
+
+
+def _lens(x):
+    return None if x is None else torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _bits(x):
+    return x.contiguous().view(torch.int16 if x.dtype == BF else torch.int32)
+
+
+# (dtype, B, Bk, H, Hkv, T, S, D, lens)
+CASES = [
+    (BF, 1, 1, 1, 1, 1, 1, 64, None),
+    (FP, 1, 1, 1, 1, 1, 1, 32, None),
+    (BF, 2, 2, 4, 2, 1, 129, 64, [129, 5]),
+    (BF, 3, 3, 8, 1, 1, 1000, 128, [1000, 1, 0]),
+    (FP, 2, 2, 4, 4, 3, 300, 128, [77, 300]),
+    (BF, 2, 2, 2, 2, 33, 31, 32, None),
+    (BF, 1, 1, 4, 2, 130, 65, 64, None),
+    (FP, 2, 2, 4, 1, 37, 129, 64, [0, 128]),
+    (FP, 1, 1, 2, 2, 161, 40, 32, [33]),
+    (BF, 2, 2, 8, 2, 96, 257, 128, [256, 33]),
+    (FP, 1, 1, 2, 1, 70, 200, 128, None),
+    (BF, 5, 1, 4, 2, 40, 100, 64, None),
+    (BF, 3, 1, 2, 1, 1, 2100, 64, [2049]),
+    (FP, 4, 1, 4, 4, 9, 70, 32, [64]),
+    (BF, 2, 2, 2, 2, 3, 5000, 32, [4999, 130]),
+    (BF, 1, 1, 8, 8, 1030, 70, 64, None),
+    (FP, 3, 1, 2, 2, 600, 33, 128, [0]),
+    (BF, 2, 2, 2, 2, 64, 64, 128, [-7, 900]),  # clamped to 0 and S
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(str(x).replace("torch.", "") for x in c))
+def test_forward_and_gradients(case):
+    dtype, B, Bk, H, Hkv, T, S, D, lens = case
+    print(case, flush=True)
+    q, k, v, dO = _inputs(*case[:8])
+    n = _lens(lens)
+    keep = None
+    if n is not None:
+        m = n.clamp(0, S)
+        keep = R.lens_mask(m.expand(B) if Bk == 1 else m, T, S)
+        for b in range(Bk):  # what is behind the lengths is not read
+            k[b, :, m[b]:], v[b, :, m[b]:] = math.nan, math.inf
+    ref = R.attention(q, k, v, dO, keep)
+    o, lse = F.fibattn_cross_forward(q, k, v, n)
+    R.check({"o": o, "lse": lse}, ref, "forward")
+    out = [torch.full_like(x, math.nan) for x in (q, k, k)]
+    dq, dk, dv = F.fibattn_cross_backward(q, k, v, o, lse, dO, n, dq=out[0], dk=out[1], dv=out[2])
+    R.check({"dq": dq, "dk": dk, "dv": dv}, ref, "backward")
+    again = F.fibattn_cross_forward(q, k, v, n)[0]
+    more = F.fibattn_cross_backward(q, k, v, o, lse, dO, n)
+    for a, b in zip((o, dq, dk, dv), (again, *more)):
+        assert torch.equal(_bits(a), _bits(b)), "two runs differ"
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_placements(dtype, D):
+    """q, k, v, o, dO and the gradients inside larger buffers; what is around them stays."""
+    B, H, Hkv, T, S = 2, 4, 2, 67, 150
+    print(dtype, D, flush=True)
+    qb = torch.full((B, T + 3, H, D), math.nan, device="cuda", dtype=dtype)
+    kvb = torch.full((B, S + 5, 2, Hkv, D), math.nan, device="cuda", dtype=dtype)
+    q0, k0, v0, dO0 = _inputs(dtype, B, B, H, Hkv, T, S, D, seed=20)
+    q = qb[:, 1:T + 1].transpose(1, 2)
+    k, v = (kvb[:, 2:S + 2, n].transpose(1, 2) for n in range(2))
+    q.copy_(q0), k.copy_(k0), v.copy_(v0)
+    dO = dO0.transpose(1, 2).contiguous().transpose(1, 2)
+    ob, dqb, dkvb = qb.clone().fill_(7.0), qb.clone().fill_(7.0), kvb.clone().fill_(7.0)
+    o, dq = (x[:, 1:T + 1].transpose(1, 2) for x in (ob, dqb))
+    dk, dv = (dkvb[:, 2:S + 2, n].transpose(1, 2) for n in range(2))
+    n = _lens([S, S - 30])
+    o, lse = F.fibattn_cross_forward(q, k, v, n, o=o)
+    F.fibattn_cross_backward(q, k, v, o, lse, dO, n, dq=dq, dk=dk, dv=dv)
+    o1, lse1 = F.fibattn_cross_forward(q0, k0, v0, n)
+    want = F.fibattn_cross_backward(q0, k0, v0, o1, lse1, dO0, n)
+    for a, b in zip((o, lse, dq, dk, dv), (o1, lse1, *want)):
+        assert torch.equal(_bits(a), _bits(b))
+    for x, a, e in ((ob, 1, T + 1), (dqb, 1, T + 1), (dkvb, 2, S + 2)):
+        assert bool((x[:, :a] == 7.0).all()) and bool((x[:, e:] == 7.0).all())
+
+
+def test_broadcast_strides():
+    """Heads and batch entries expanded by stride 0."""
+    q, k, v, _ = _inputs(BF, 3, 1, 4, 1, 20, 90, 64, seed=30)
+    ke, ve = k.expand(3, 4, 90, 64), v.expand(3, 4, 90, 64)
+    o, lse = F.fibattn_cross_forward(q, ke, ve)
+    R.check({"o": o, "lse": lse}, R.attention(q, ke.contiguous(), ve.contiguous()), "expanded")
+
+
+def test_not_finite_values():
+    q, k, v, _ = _inputs(BF, 1, 1, 2, 2, 40, 100, 64, seed=40)
+    v[0, 0, 3, 5], v[0, 1, 99, 0] = math.inf, -math.inf
+    o, _ = F.fibattn_cross_forward(q, k, v)
+    assert bool((o[0, 0, :, 5] == math.inf).all()) and bool((o[0, 1, :, 0] == -math.inf).all())
+    assert int(torch.isfinite(o).sum()) == o.numel() - 2 * 40
+    q[0, 0, 7, 1] = math.nan
+    o, lse = F.fibattn_cross_forward(q, k, v)
+    assert bool(torch.isnan(o[0, 0, 7]).all()) and bool(torch.isnan(lse[0, 0, 7]))
+    assert int(torch.isnan(o).sum()) == 64 and int(torch.isnan(lse).sum()) == 1
+
+
+def test_large_logits():
+    """Weights that all but one row round to 0, and a maximum that keeps moving."""
+    q, k, v, dO = _inputs(FP, 1, 1, 1, 1, 64, 512, 64, seed=50)
+    k = k * torch.linspace(0.1, 40.0, 512, device="cuda")[None, None, :, None]
+    ref = R.attention(q, k, v, dO)
+    o, lse = F.fibattn_cross_forward(q, k, v)
+    R.check({"o": o, "lse": lse}, ref, "large logits")
+    dq, dk, dv = F.fibattn_cross_backward(q, k, v, o, lse, dO)
+    R.check({"dq": dq, "dk": dk, "dv": dv}, ref, "large logits")
+
+
+def test_gradient_against_differences():
+    """<grad, x> against (f(+h) - f(-h)) / 2h of f = <dO, o> in float32, along a random
+    direction.  h = 2^-6: the third derivative's term is below h^2 times the gradient's
+    scale, and the difference of two float32 sums of 1e3 terms is good to 1e-6 / h."""
+    q, k, v, dO = _inputs(FP, 2, 2, 4, 2, 17, 45, 32, seed=60)
+    n = _lens([45, 20])
+    o, lse = F.fibattn_cross_forward(q, k, v, n)
+    grads = F.fibattn_cross_backward(q, k, v, o, lse, dO, n)
+    h = 2.0 ** -6
+    for a, g in enumerate(grads):
+        x = _normal(70 + a, *g.shape)
+        x = x / x.norm() * 4
+
+        def f(sign):
+            y = [q, k, v]
+            y[a] = y[a] + sign * h * x
+            return float((F.fibattn_cross_forward(*y, n)[0].double() * dO.double()).sum())
+
+        d = (f(1) - f(-1)) / (2 * h)
+        want = float((g.double() * x.double()).sum())
+        scale = float((g.double() ** 2).sum().sqrt()) * 4
+        assert abs(d - want) <= 40 * h * h * scale + 1e-3, (a, d, want)
+
+
+# (dtype, B, H, Hkv, T, P, S, D, lens)
+PREFIX = [
+    (BF, 2, 4, 2, 1, 64, 16, 64, [3, 16]),
+    (BF, 1, 1, 1, 1, 1, 1, 32, None),
+    (BF, 5, 8, 2, 4, 300, 50, 128, [4, 50, 2, 0, 17]),
+    (FP, 3, 4, 4, 2, 77, 130, 64, [130, 1, 99]),
+    (BF, 40, 4, 1, 1, 2100, 700, 64, None),
+    (FP, 2, 2, 1, 40, 100, 90, 32, [90, 39]),
+    (BF, 2, 8, 1, 33, 129, 300, 64, [300, 40]),
+    (FP, 2, 4, 2, 5, 600, 1000, 128, [1000, 700]),
+]
+
+
+@pytest.mark.parametrize("case", PREFIX, ids=lambda c: "-".join(str(x).replace("torch.", "") for x in c))
+def test_prefix(case):
+    dtype, B, H, Hkv, T, P, S, D, lens = case
+    print(case, flush=True)
+    q, k, v, _ = _inputs(dtype, B, B, H, Hkv, T, S, D, seed=80)
+    _, kp, vp, _ = _inputs(dtype, B, 1, H, Hkv, T, P, D, seed=90)
+    n = _lens(lens)
+    m = torch.full((B,), S, device="cuda") if n is None else n
+    for b in range(B):  # rows behind the lengths are not read
+        k[b, :, m[b]:], v[b, :, m[b]:] = math.nan, math.inf
+    keep = torch.cat([torch.ones((B, T, P), dtype=torch.bool, device="cuda"), R.newest_mask(m, T, S)], dim=2)
+    ref = R.attention(q, torch.cat([kp.expand(B, -1, -1, -1), k], 2), torch.cat([vp.expand(B, -1, -1, -1), v], 2),
+                      keep=keep)
+    o, lse = F.fibattn_prefix_forward(q, kp, vp, k, v, n)
+    R.check({"o": o, "lse": lse}, ref, "prefix")
+    # views: the caches as [B,S,Hkv,D] and [P,2,Hkv,D]
+    cache = torch.stack([k, v]).permute(0, 1, 3, 2, 4).contiguous()
+    pre = torch.stack([kp[0], vp[0]]).permute(2, 0, 1, 3).contiguous()
+    views = [x.permute(1, 0, 2)[None] for x in (pre[:, 0], pre[:, 1])] + [x.transpose(1, 2) for x in cache]
+    o2, lse2 = F.fibattn_prefix_forward(q.transpose(1, 2).contiguous().transpose(1, 2), *views, n)
+    assert torch.equal(_bits(o), _bits(o2)) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("dtype,T,G", [(BF, 4, 2), (FP, 3, 1), (BF, 40, 4)])
+def test_prefix_values_of_later_tokens(dtype, T, G):
+    """A value that is not finite in a row that only later tokens read stays with them."""
+    B, Hkv, P, S, D = 2, 2, 70, 64, 64
+    q, k, v, _ = _inputs(dtype, B, B, Hkv * G, Hkv, T, S, D, seed=100)
+    _, kp, vp, _ = _inputs(dtype, B, 1, Hkv * G, Hkv, T, P, D, seed=110)
+    n = _lens([S, S - 5])
+    clean, _ = F.fibattn_prefix_forward(q, kp, vp, k, v, n)
+    v[0, 0, S - 1] = math.nan  # the newest token of sequence 0, key/value head 0
+    k[1, 1, S - 6, 3] = math.nan  # of sequence 1, head 1
+    o, lse = F.fibattn_prefix_forward(q, kp, vp, k, v, n)
+    keep = torch.cat([torch.ones((B, T, P), dtype=torch.bool, device="cuda"), R.newest_mask(n, T, S)], dim=2)
+    last = torch.zeros((B, Hkv * G, T), dtype=torch.bool, device="cuda")
+    last[0, :G, T - 1] = last[1, G:, T - 1] = True
+    assert bool(torch.isnan(o[last]).all()) and bool(torch.isfinite(o[~last]).all())
+    ref = R.attention(q, torch.cat([kp.expand(B, -1, -1, -1), k.nan_to_num()], 2),
+                      torch.cat([vp.expand(B, -1, -1, -1), v.nan_to_num()], 2), keep=keep)
+    bad = (o.double() - ref["o"]).abs() > ref["e_o"]
+    assert not bool(bad[~last].any())
+    assert torch.equal(clean[0, G:], o[0, G:])
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_join(dtype, D):
+    B, H, T = 2, 3, 37
+    oa, ob = _normal(120, B, H, T, D, dtype=dtype), _normal(121, B, T, H, D, dtype=dtype).transpose(1, 2)
+    la, lb = 3 * _normal(122, B, H, T), 3 * _normal(123, B, H, T)
+    la[0, 0, :5], lb[0, 0, 4:9] = -math.inf, -math.inf  # position 4: neither
+    oa[0, 0, :5], ob[0, 0, 4:9] = math.nan, math.inf
+    both = torch.logaddexp(la.double(), lb.double())
+    safe = torch.where(both == -math.inf, torch.zeros_like(both), both)
+    wa, wb = (torch.exp(x.double() - safe)[..., None] for x in (la, lb))
+    a, b = (torch.where(w > 0, w * x.double(), torch.zeros_like(w)) for w, x in ((wa, oa), (wb, ob)))
+    # weights, products and the sum in float32: 16 roundings of 2^-24 on |a| + |b|, exponents
+    # up to 16 in magnitude with the same relative error; then the stored rounding
+    ref = {"o": a + b, "lse": both, "e_o": 2.0 ** -19 * (a.abs() + b.abs()) + R.STORE[dtype] * (a + b).abs(),
+           "e_lse": 2.0 ** -21 * (safe.abs() + 1)}
+    o, lse = F.fibattn_join(oa, la, ob, lb)
+    R.check({"o": o, "lse": lse}, ref, "join")
+    F.fibattn_join(oa, la, ob, lb, o=oa, lse=la)
+    assert torch.equal(_bits(o), _bits(oa)) and torch.equal(lse, la)
+
+
+@pytest.mark.parametrize("dtype,H,Hkv,D", [(BF, 8, 2, 64), (FP, 4, 4, 32), (BF, 4, 4, 128)])
+def test_sparse_layer_with_shared_rows(dtype, H, Hkv, D):
+    """A sparse self-attention layer whose queries also read M rows shared by the batch, in
+    one softmax: forward, join and both backwards, against 64 bits of the whole."""
+    B, T, M, W = 2, 200, 40, 8
+    base = schedules.FIB15
+    q, k, v, dO = _inputs(dtype, B, B, H, Hkv, T, T, D, seed=130)
+    _, km, vm, _ = _inputs(dtype, B, 1, H, Hkv, T, M, D, seed=140)
+    o1, l1 = F.fibattn_forward(q, k, v, W, base, 1.0)
+    o2, l2 = F.fibattn_cross_forward(q, km, vm)
+    o, lse = F.fibattn_join(o1, l1, o2, l2)
+    dq1, dk, dv, _ = F.fibattn_backward(q, k, v, o, lse, dO, W, base, 1.0)
+    dq2, dkm, dvm = F.fibattn_cross_backward(q, km, vm, o, lse, dO)
+    i, j = torch.arange(T, device="cuda")[:, None], torch.arange(T, device="cuda")[None]
+    own = ((i >= j) & (i - j <= W))
+    for f in base:
+        own |= (i - j) == f
+    keep = torch.cat([own, torch.ones((T, M), dtype=torch.bool, device="cuda")], 1)[None].expand(B, T, T + M)
+    kk, vv = (torch.cat([x, y.expand(B, -1, -1, -1)], 2) for x, y in ((k, km), (v, vm)))
+    ref = R.attention(q, kk, vv, dO, keep)
+    # the parts' o are stored before they are joined, and each dq before the sum: one more
+    # rounding of each; the sparse kernels round their weights the same way
+    us = R.STORE[dtype]
+    ref["e_o"] = 2 * ref["e_o"] + 2 * us * ref["o"].abs()
+    for n in ("dq", "dk", "dv"):
+        ref["e_" + n] = 3 * ref["e_" + n] + 2 * us * ref[n].abs()
+    dqs = dq1.double() + dq2.double()
+    ref["e_dq"] += us * (dq1.double().abs() + dq2.double().abs())
+    R.check({"o": o, "lse": lse}, ref, "joined")
+    for n, a, c in (("dk", dk, dkm), ("dv", dv, dvm)):
+        ref[n + "m"], ref["e_" + n + "m"] = (x[:, :, T:].sum(0, keepdim=True) for x in (ref[n], ref["e_" + n]))
+        ref[n], ref["e_" + n] = ref[n][:, :, :T], ref["e_" + n][:, :, :T]
+        R.check({n: a, n + "m": c}, ref, "joined")
+    R.check({"dq": dqs}, ref, "joined")
+
+
+def test_streams_and_graph():
+    """A call on another stream, and a captured chain replayed beside eager calls."""
+    B, H, Hkv, T, S, D = 2, 8, 2, 1, 1200, 64
+    q, k, v, dO = _inputs(BF, B, B, H, Hkv, T, S, D, seed=150)
+    _, kp, vp, _ = _inputs(BF, B, 1, H, Hkv, T, 900, D, seed=160)
+    n = _lens([1200, 700])
+
+    def chain():
+        o, lse = F.fibattn_cross_forward(q, k, v, n)
+        dq, dk, dv = F.fibattn_cross_backward(q, k, v, o, lse, dO, n)
+        o2, lse2 = F.fibattn_prefix_forward(q, kp, vp, k, v, n)
+        return (*F.fibattn_join(o, lse, o2, lse2), dq, dk, dv)
+
+    want = [x.clone() for x in chain()]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    o, lse = F.fibattn_cross_forward(q, k, v, n, stream=side)
+    with torch.cuda.stream(side):
+        got = chain()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert torch.equal(o, F.fibattn_cross_forward(q, k, v, n)[0])
+    for a, b in zip(got, want):
+        assert torch.equal(_bits(a), _bits(b))
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = chain()
+    for r in range(3):
+        q.copy_(_normal(170 + r, B, H, T, D, dtype=BF))
+        n.copy_(_lens([3 + 400 * r, 1200 - 400 * r]))
+        want = [x.clone() for x in chain()]
+        g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(_bits(a), _bits(b)), r
+
+
+def test_workspace_of_the_caller():
+    B, H, Hkv, T, S, D = 1, 4, 4, 1, 4000, 64
+    q, k, v, dO = _inputs(BF, B, B, H, Hkv, T, S, D, seed=180)
+    need = F.fibattn_cross_workspace_bytes(B, B, H, Hkv, T, S, D)
+    assert need > 0
+    ws = torch.full((need,), 255, device="cuda", dtype=torch.uint8)
+    o, lse = F.fibattn_cross_forward(q, k, v, workspace=ws)
+    assert torch.equal(o, F.fibattn_cross_forward(q, k, v)[0])
+    with pytest.raises(F.FibattnError) as e:
+        F.fibattn_cross_forward(q, k, v, workspace=ws[:-16])
+    assert e.value.status == 3
+    need = F.fibattn_cross_backward_workspace_bytes(B, B, H, Hkv, T, S, D)
+    ws = torch.full((need,), 255, device="cuda", dtype=torch.uint8)
+    got = F.fibattn_cross_backward(q, k, v, o, lse, dO, workspace=ws)
+    for a, b in zip(got, F.fibattn_cross_backward(q, k, v, o, lse, dO)):
+        assert torch.equal(_bits(a), _bits(b))
+
+
+def test_long_states():
+    """Offsets of the states past 2^32 bytes: two heads, the second one 4.3 GB on."""
+    S, D = 1 << 24, 64
+    k = torch.empty((1, 2, S + 300000, D), device="cuda", dtype=BF)
+    k = k[:, :, :S]
+    k[0, 1].normal_()
+    k[0, 0].zero_()
+    q = _normal(190, 1, 2, 1, D, dtype=BF)
+    k[0, 1, S - 1] = 30 * q[0, 1, 0] / q[0, 1, 0].float().norm()  # the row that the query finds
+    o, lse = F.fibattn_cross_forward(q, k, k)
+    # head 0: zero keys, lse = log S and o = 0; head 1: in 64 bits, in pieces
+    assert bool((o[0, 0] == 0).all()) and abs(float(lse[0, 0, 0]) - math.log(S)) < 1e-5
+    total = torch.zeros((), dtype=torch.float64, device="cuda")
+    y, size = torch.zeros((D,), dtype=torch.float64, device="cuda"), torch.zeros((D,), dtype=torch.float64, device="cuda")
+    for a in range(0, S, 1 << 21):
+        x = k[0, 1, a:a + (1 << 21)].double()
+        w = torch.exp(x @ q[0, 1, 0].double() / 8 - 20)
+        total += w.sum()
+        y += w @ x
+        size += w @ x.abs()
+    y, size = y / total, size / total
+    z = float(torch.log(total) + 20)
+    # a piece sums up to S / 64 rows a wave's lane after the other: 2^18 2^-24 of the sum
+    assert abs(float(lse[0, 1, 0]) - z) < 2.0 ** -6
+    assert bool(((o[0, 1, 0].double() - y).abs() <= (2.0 ** -8 + 2.0 ** -6) * size + 2.0 ** -8 * y.abs()).all())
