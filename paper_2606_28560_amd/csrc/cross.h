@@ -24,7 +24,7 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short i16x4_t __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2_t __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
 
 template <typename S> struct FragOf;
 template <> struct FragOf<uint16_t> { typedef bf16x8_t type; };
@@ -50,20 +50,39 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 
 // Values 8a .. 8a + 7 of a result as the operand of a step over its rows 16a .. 16a + 15.
-// bfloat16: each weight is rounded once, by at most 2^-8 of itself, as the stored values
-// it multiplies were; the sums stay in float32.
-__device__ __forceinline__ void to_frag(const f32x16_t &x, int a, bf16x8_t &f) {
-    uint4 u;
-    u.x = pack2(x[8 * a], x[8 * a + 1]);
-    u.y = pack2(x[8 * a + 2], x[8 * a + 3]);
-    u.z = pack2(x[8 * a + 4], x[8 * a + 5]);
-    u.w = pack2(x[8 * a + 6], x[8 * a + 7]);
-    f = __builtin_bit_cast(bf16x8_t, u);
-}
-__device__ __forceinline__ void to_frag(const f32x16_t &x, int a, f32x8_t &f) {
+// A weight rounded to bfloat16 once is off by up to 2^-8, as much again as the rounding of a
+// stored output: bfloat16 weights go as two operands, the rounded weight and the rounded
+// rest (a dot product with -1 and 0 takes the difference, which is exact), good to 2^-16.
+template <typename S> struct Weights;
+template <> struct Weights<uint16_t> {
+    bf16x8_t hi, lo;
+    __device__ __forceinline__ Weights(const f32x16_t &x, int a) {
+        uint32_t h[4], l[4];
+        uint32_t first = 0x0000bf80u, second = 0xbf800000u;  // (-1, 0), (0, -1): in registers, since
+        asm("" : "+s"(first), "+s"(second));  // as constants of the instruction they are read otherwise
 #pragma unroll
-    for (int s = 0; s < 8; ++s) f[s] = x[8 * a + s];
-}
+        for (int i = 0; i < 4; ++i) {
+            const float u = x[8 * a + 2 * i], v = x[8 * a + 2 * i + 1];
+            h[i] = pack2(u, v);
+            const bf16x2_t p = __builtin_bit_cast(bf16x2_t, h[i]);
+            l[i] = pack2(__builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf16x2_t, first), u, false),
+                         __builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf16x2_t, second), v, false));
+        }
+        hi = __builtin_bit_cast(bf16x8_t, make_uint4(h[0], h[1], h[2], h[3]));
+        lo = __builtin_bit_cast(bf16x8_t, make_uint4(l[0], l[1], l[2], l[3]));
+    }
+    __device__ __forceinline__ f32x16_t add(const bf16x8_t &f, const f32x16_t &c) const {
+        return mma(f, hi, mma(f, lo, c));
+    }
+};
+template <> struct Weights<float> {
+    f32x8_t w;
+    __device__ __forceinline__ Weights(const f32x16_t &x, int a) {
+#pragma unroll
+        for (int s = 0; s < 8; ++s) w[s] = x[8 * a + s];
+    }
+    __device__ __forceinline__ f32x16_t add(const f32x8_t &f, const f32x16_t &c) const { return mma(f, w, c); }
+};
 
 // The other half's value of the same row (lanes l and l ^ 32) joined with the lane's own.
 __device__ __forceinline__ float half_max(float x) {
@@ -77,9 +96,52 @@ __device__ __forceinline__ float half_sum(float x) {
 
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Waits until at most N of this wave's vector-memory operations are outstanding.
-template <int N> __device__ __forceinline__ void wait_loads() {
-    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+// Waits until at most N of this wave's vector-memory operations are outstanding; no access to
+// memory moves across.
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+// Waits until this wave's reads of LDS are done.
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
+
+__device__ __forceinline__ uint32_t lds_address(const void *p) {
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
+}
+
+// A value that is the same in every lane.
+__device__ __forceinline__ uint32_t uniform(uint64_t x) {
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)x);
+}
+
+// The buffer loads that write LDS directly: each lane's 4 or 16 bytes at byte `off` of the
+// buffer go to LDS byte `to` (the same in every lane) + the lane's place; past the buffer's end
+// zeros do.  Written in assembly, without a register loaded, so that reads of other LDS do not
+// wait for them: their own readers do so by wait_loads and, across waves, a barrier.  s_nop 4:
+// the wait states between a vector write of a scalar register (a spilled one restored, say) and
+// its use by a load; s_nop 0: between m0 and a load to LDS.
+__device__ __forceinline__ void load_lds4(uint32_t to, u32x4_t buf, int off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
+                 :
+                 : "s"(to), "v"(off), "s"(buf)
+                 : "memory");
+}
+__device__ __forceinline__ void load_lds16(uint32_t to, u32x4_t buf, int off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(to), "v"(off), "s"(buf)
+                 : "memory");
+}
+// Four of them, `step` bytes of LDS apart.
+__device__ __forceinline__ void load_lds16(uint32_t to, uint32_t step, u32x4_t buf, const int *off) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %2, %6, 0 offen lds\n\t"
+                 "s_add_u32 m0, m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %3, %6, 0 offen lds\n\t"
+                 "s_add_u32 m0, m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %4, %6, 0 offen lds\n\t"
+                 "s_add_u32 m0, m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %5, %6, 0 offen lds"
+                 :
+                 : "s"(to), "s"(step), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(buf)
+                 : "memory", "scc");
+}
+__device__ __forceinline__ u32x4_t buffer_of(const void *src, uint32_t bytes) {
+    const uint64_t base = (uint64_t)src;
+    return u32x4_t{uniform(base), uniform((base >> 32) & 0xffffu), uniform(bytes), 0x00027000u};
 }
 
 // Rows of D values staged in LDS: row-major, the 16-byte chunks of a row exchanged by an XOR
@@ -96,24 +158,30 @@ template <typename S, int D> struct Tile {
     }
 
     // Rows [0, N) at `src`, `stride` bytes apart (64 of them below 2^31 bytes), to `dst` by the
-    // buffer loads that write LDS directly.  Rows from `valid` (>= 1) on are read past the buffer's
-    // end and come back as zeros: a weight of 0 never meets an infinity there.  The loads are
-    // shared by NW waves; this is wave w.
+    // buffer loads that write LDS directly.  Rows from `valid` (>= 1) on are read past the
+    // buffer's end and come back as zeros: a weight of 0 never meets an infinity there.  The
+    // loads are shared by NW waves; this is wave w.
     template <int N, int NW>
     __device__ __forceinline__ static void stage(char *dst, const char *src, long long stride, int valid, int w) {
-        constexpr int loads = N / kRowsPerLoad;
+        constexpr int loads = N / kRowsPerLoad, each = (loads + NW - 1) / NW;
         const int lane = threadIdx.x & 63;
         const int rr = lane / kChunks, pc = lane % kChunks;
         const int st = (int)stride;
-        const __amdgpu_buffer_rsrc_t buf =
-            __builtin_amdgcn_make_buffer_rsrc((void *)src, 0, (min(valid, N) - 1) * st + kRow, 0x00027000);
+        const u32x4_t buf = buffer_of(src, (uint32_t)((min(valid, N) - 1) * st + kRow));
+        const uint32_t to = uniform(lds_address(dst) + 1024 * w);
+        int off[each];
 #pragma unroll
-        for (int a = 0; a < (loads + NW - 1) / NW; ++a) {
-            const int blk = a * NW + w;
-            if (loads % NW && blk >= loads) break;
-            const int r = blk * kRowsPerLoad + rr;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (__attribute__((address_space(3))) void *)(dst + 1024 * blk), 16,
-                                                     r < valid ? r * st + 16 * (pc ^ swz(r)) : 0x7fffff00, 0, 0, 0);
+        for (int a = 0; a < each; ++a) {
+            const int r = (a * NW + w) * kRowsPerLoad + rr;
+            off[a] = r < valid ? r * st + 16 * (pc ^ swz(r)) : 0x7fffff00;
+        }
+        if constexpr (each % 4 == 0) {
+#pragma unroll
+            for (int a = 0; a < each; a += 4) load_lds16(to + 1024 * NW * a, 1024 * NW, buf, off + a);
+        } else {
+#pragma unroll
+            for (int a = 0; a < each; ++a)
+                if (loads % NW == 0 || a * NW + w < loads) load_lds16(to + 1024 * NW * a, buf, off[a]);
         }
     }
 

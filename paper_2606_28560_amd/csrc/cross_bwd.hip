@@ -53,13 +53,12 @@ __device__ __forceinline__ void dq_step(const char *__restrict kt, const char *_
     for (int i = 0; i < 16; ++i) s[i] = ex2(fmaf(s[i], scale, -w.lse2)) * (u[i] - w.delta);
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
-        Frag<S> p;
-        to_frag(s, a, p);
+        const Weights<S> p(s, a);
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) {
             Frag<S> f;
             X::operand_t(kt, row0 + 16 * a, dt, f);
-            w.acc[dt] = mma(f, p, w.acc[dt]);
+            w.acc[dt] = p.add(f, w.acc[dt]);
         }
     }
 }
@@ -193,7 +192,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dkdv_kernel(Gradi
                                      (const char *)((const S *)a.g + b * a.lg.sb + hh * a.lg.sh + t0 * a.lg.st), gs,
                                      a.T - t0, wv);
             if (wv == 3)
-                __builtin_amdgcn_global_load_lds(a.stats + stat_at(a, b, hh, t0) + lane, dst + 2 * TB, 4, 0, 0);
+                load_lds4(uniform(lds_address(dst + 2 * TB)), buffer_of(a.stats + stat_at(a, b, hh, t0), 256), 4 * lane);
         };
         auto fetch_all = [&](int i, int half) {
 #pragma unroll
@@ -238,16 +237,14 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dkdv_kernel(Gradi
                 }
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    Frag<S> p, ds;
-                    to_frag(s, x, p);
-                    to_frag(u, x, ds);
+                    const Weights<S> p(s, x), ds(u, x);
 #pragma unroll
                     for (int dt = 0; dt < D / 32; ++dt) {
                         Frag<S> f;
                         X::operand_t(gt, 16 * x, dt, f);
-                        dv[dt] = mma(f, p, dv[dt]);
+                        dv[dt] = p.add(f, dv[dt]);
                         X::operand_t(qt, 16 * x, dt, f);
-                        dk[dt] = mma(f, ds, dk[dt]);
+                        dk[dt] = ds.add(f, dk[dt]);
                     }
                 }
             }

@@ -102,13 +102,12 @@ template <typename S, int D>
 __device__ __forceinline__ void values(const char *vt, int row0, const f32x16_t &p, Rows<S, D> &w) {
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
-        Frag<S> pf;
-        to_frag(p, a, pf);
+        const Weights<S> pw(p, a);
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) {
             Frag<S> f;
             Tile<S, D>::operand_t(vt, row0 + 16 * a, dt, f);
-            w.acc[dt] = mma(f, pf, w.acc[dt]);
+            w.acc[dt] = pw.add(f, w.acc[dt]);
         }
     }
 }
@@ -127,6 +126,13 @@ __device__ __forceinline__ S *out_row(const Queries &a, const RowAt &at) {
     return (S *)a.o + at.b * a.lo.sb + at.h * a.lo.sh + at.t * a.lo.st;
 }
 
+// Query rows first, first + step, .. below `end` of a problem over rows [c0, c1) of the states
+// that are to be done again (end 0: none).
+struct Redo {
+    int b0, j, first, step, end, c0, c1, len;
+    long long slot;
+};
+
 // One problem's rows of the states; stage i holds rows i NT .. of k, then of v.
 template <typename S, int D> struct Source {
     const char *k, *v;
@@ -140,14 +146,10 @@ template <typename S, int D> struct Source {
     }
 };
 
-// Fetches the next stage and works on the present one.  `restrict`: the loads into the next
-// stage's LDS are not waited for by the reads of this one's.
+// The wave's work on stage i of the states.
 template <typename S, int D>
-__device__ __forceinline__ void rows_step(const char *__restrict cur, char *__restrict next, const Source<S, D> &src,
-                                          int i, bool more, int wv, int low, bool idle, float scale, Rows<S, D> &w) {
+__device__ __forceinline__ void rows_step(const char *cur, int i, int low, float scale, Rows<S, D> &w) {
     constexpr int NT = kStage<S>, NS = NT / 32, TB = NT * Tile<S, D>::kRow;
-    if (more) src.fetch(next, i + 1, wv);
-    if (idle) return;
     f32x16_t s[NS];
 #pragma unroll
     for (int e = 0; e < NS; ++e) s[e] = logits<S, D>(cur, 32 * e, w);
@@ -162,7 +164,7 @@ __device__ __forceinline__ void rows_step(const char *__restrict cur, char *__re
 
 // 128 query rows, 32 to a wave; the waves share the staged rows of the states.
 template <typename S, int D>
-__device__ __forceinline__ void rows_body(const Queries &a, const States &st, int item, char *lds) {
+__device__ __forceinline__ void rows_body(const Queries &a, const States &st, int item, char *lds, Redo &todo) {
     typedef Tile<S, D> X;
     constexpr int NT = kStage<S>, TB = NT * X::kRow;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -185,11 +187,22 @@ __device__ __forceinline__ void rows_body(const Queries &a, const States &st, in
         wait_loads<0>();
         __syncthreads();  // this stage has arrived, the one before has been read
         const int buf = (i - n0) & 1;
-        rows_step<S, D>(lds + buf * 2 * TB, lds + (buf ^ 1) * 2 * TB, src, i, i + 1 < n1, wv, low, idle, a.scale, w);
+        if (i + 1 < n1) src.fetch(lds + (buf ^ 1) * 2 * TB, i + 1, wv);
+        if (!idle) rows_step<S, D>(lds + buf * 2 * TB, i, low, a.scale, w);
     }
     const float l = half_sum(w.l), f = l == 0.f ? 0.f : 1.f / l;
-    if (!w.on) return;
     const long long slot = st.slot + piece;
+    float nan = 0.f;  // NaN if a value is (or an infinity)
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) nan = fmaf(w.acc[dt][e], 0.f, nan);
+    if (__ballot(w.on && nan != 0.f)) {
+        const int r0 = 128 * tile + 32 * wv;
+        todo = {b0, j, r0, 1, r0 + 32, n0 * NT, min(n1 * NT, len), len, slot};
+        return;
+    }
+    if (!w.on) return;
     if (lane < 32) put_lse(a, slot, w.id, w.m, l);
     if (a.part_o)
         store_cols<D>(a.part_o + (slot * a.B * a.H * a.T + w.id) * D, w.acc, f, lane >> 5);
@@ -200,7 +213,7 @@ __device__ __forceinline__ void rows_body(const Queries &a, const States &st, in
 // 32 query rows for all four waves, each on its own rows of the states (tiles of 32, one in
 // four), staged for the wave alone; joined in LDS.
 template <typename S, int D>
-__device__ __forceinline__ void keys_body(const Queries &a, const States &st, int item, char *lds) {
+__device__ __forceinline__ void keys_body(const Queries &a, const States &st, int item, char *lds, Redo &todo) {
     typedef Tile<S, D> X;
     constexpr int TB = 32 * X::kRow, OPS = 32 / X::kRowsPerLoad;
     __shared__ float stat[2][4][32];
@@ -226,7 +239,7 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
         const bool more = i + 4 < n1;
         wait_loads<OPS>();  // K is here, V may be on its way
         f32x16_t s = logits<S, D>(kt, 0, w);
-        __builtin_amdgcn_s_waitcnt(0xC07F);  // K has been read
+        wait_lds();  // K has been read
         if (more) X::template stage<32, 1>(kt, kp + 32 * (i + 4) * ks, ks, len - 32 * (i + 4), 0);
         if (32 * (i + 1) > low) mask<S, D>(s, 32 * i, w);
         weights<S, D, 1>(&s, a.scale, w);
@@ -235,7 +248,7 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
         else
             wait_loads<0>();
         values<S, D>(vt, 0, s, w);
-        __builtin_amdgcn_s_waitcnt(0xC07F);  // V has been read
+        wait_lds();  // V has been read
         if (more) X::template stage<32, 1>(vt, vp + 32 * (i + 4) * vs, vs, len - 32 * (i + 4), 0);
     }
     // the waves' results of each row, in the order of the waves
@@ -250,6 +263,7 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
     __syncthreads();
     const long long slot = st.slot + piece;
     constexpr int V = 4, per = D / V;  // lanes to a row
+    float nan = 0.f;  // NaN if a value is (or an infinity)
     for (int e = threadIdx.x; e < 32 * per; e += 256) {
         const int r = e / per, d = e % per * V;
         if (32 * tile + r >= st.rows) continue;
@@ -266,6 +280,7 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
             y += *reinterpret_cast<const f32x4_t *>(part + (32 * x + r) * D + d) * f;
         }
         const float f = sum == 0.f ? 0.f : 1.f / sum;
+        nan = fmaf(y[0] + y[1] + y[2] + y[3], 0.f, nan);
         const RowAt at = row_at(a, b0, j, 32 * tile + r);
         const long long id = ((long long)at.b * a.H + at.h) * a.T + at.t;
         if (d == 0) put_lse(a, slot, id, m, sum);
@@ -279,24 +294,8 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
                 *reinterpret_cast<uint2 *>(row) = make_uint2(pack2(y[0] * f, y[1] * f), pack2(y[2] * f, y[3] * f));
         }
     }
-}
-
-// Whether rows of the states that only some queries read hold an infinity or NaN among their
-// values: a weight of 0 times such a value would reach the queries that do not read it.
-template <typename S, int D>
-__device__ __forceinline__ bool not_finite(const Queries &a, const States &st, int item) {
-    const int prob = item / st.tiles / st.splits, b0 = prob / a.Hkv, j = prob % a.Hkv;
-    const int len = states_len(st, b0), low = max(len - a.T + 1, 0);
-    const S *v = (const S *)st.v + b0 * st.lv.sb + j * st.lv.sh;
-    constexpr int N = 16 / (int)sizeof(S), per = D / N;
-    int bad = 0;
-    for (int e = threadIdx.x; e < (len - low) * per; e += 256) {
-        float x[N];
-        Vec<S>::load(v + (low + e / per) * st.lv.st + e % per * N, x);
-#pragma unroll
-        for (int i = 0; i < N; ++i) bad |= !(fabsf(x[i]) < INFINITY);
-    }
-    return __syncthreads_or(bad);
+    if (__syncthreads_or(nan != 0.f))
+        todo = {b0, j, 32 * tile + wv, 4, 32 * tile + 32, 32 * n0, min(32 * n1, len), len, slot};
 }
 
 __device__ __forceinline__ float value_of(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
@@ -304,30 +303,31 @@ __device__ __forceinline__ float value_of(float x) { return x; }
 __device__ __forceinline__ void put_value(uint16_t *p, float x) { *p = (uint16_t)f32_to_bf16(x); }
 __device__ __forceinline__ void put_value(float *p, float x) { *p = x; }
 
-// A wave per query row, one row of the states at a time, and only those the query reads.
-// For causal states with values that are not finite (not_finite).
+// The rows of `todo`, each by the whole wave, one row of the states at a time and only those
+// it reads.
+//
+// The tiles multiply what a query does not read by a weight of 0, and a weight's bfloat16 rest
+// may be 0 or negative: with an infinity or NaN among the values either makes a NaN of what
+// is not one.  Rows whose tiles end in NaN are done again here, where nothing unread enters.
 template <typename S, int D>
-__device__ __forceinline__ void plain_body(const Queries &a, const States &st, int item, int tile_rows) {
+__device__ __forceinline__ void plain_rows(const Queries &a, const States &st, const Redo &todo) {
+    const int b0 = todo.b0, j = todo.j, len = todo.len;
+    const long long slot = todo.slot;
     constexpr int N = (D + 63) / 64;
-    const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-    const int tile = item % st.tiles, piece = item / st.tiles % st.splits, prob = item / st.tiles / st.splits;
-    const int b0 = prob / a.Hkv, j = prob % a.Hkv;
-    const int len = states_len(st, b0);
+    const int lane = threadIdx.x & 63;
     const S *k = (const S *)st.k + b0 * st.lk.sb + j * st.lk.sh, *v = (const S *)st.v + b0 * st.lv.sb + j * st.lv.sh;
-    const int n0 = (int)((long long)len * piece / st.splits), n1 = (int)((long long)len * (piece + 1) / st.splits);
-    const long long slot = st.slot + piece;
-    for (int r = tile * tile_rows + wv; r < min((tile + 1) * tile_rows, st.rows); r += 4) {
+    for (int r = todo.first; r < min(todo.end, st.rows); r += todo.step) {
         const RowAt at = row_at(a, b0, j, r);
         const long long id = ((long long)at.b * a.H + at.h) * a.T + at.t;
         const S *q = (const S *)a.q + at.b * a.lq.sb + at.h * a.lq.sh + at.t * a.lq.st;
-        const int lim = min(st.causal ? len - a.T + 1 + at.t : len, n1);
+        const int lim = min(st.causal ? len - a.T + 1 + at.t : len, todo.c1);
         float x[N], y[N], m = -INFINITY, l = 0.f;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             x[n] = lane + 64 * n < D ? value_of(q[lane + 64 * n]) : 0.f;
             y[n] = 0.f;
         }
-        for (int c = n0; c < lim; ++c) {
+        for (int c = todo.c0; c < lim; ++c) {
             float s = 0.f;
 #pragma unroll
             for (int n = 0; n < N; ++n)
@@ -366,13 +366,13 @@ __global__ __launch_bounds__(256, 2) void cross_fwd_kernel(Queries a, States s0,
     const bool first = b < n0;
     const States st = first ? s0 : s1;
     const int item = first ? xcd_item(b, n0) : xcd_item(b - n0, n - n0);
-    const bool by_keys = first ? by_keys0 : by_keys1;
-    if (st.causal && not_finite<S, D>(a, st, item))
-        plain_body<S, D>(a, st, item, by_keys ? 32 : 128);
-    else if (by_keys)
-        keys_body<S, D>(a, st, item, lds);
+    Redo todo;
+    todo.end = 0;
+    if (first ? by_keys0 : by_keys1)
+        keys_body<S, D>(a, st, item, lds, todo);
     else
-        rows_body<S, D>(a, st, item, lds);
+        rows_body<S, D>(a, st, item, lds, todo);
+    if (todo.end) plain_rows<S, D>(a, st, todo);
 }
 
 // Partial results of a row: o = sum_i exp(lse_i - lse) o_i, lse = log sum_i exp(lse_i).  A
