@@ -97,8 +97,11 @@ __device__ __forceinline__ float half_sum(float x) {
 __device__ __forceinline__ float ex2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Waits until at most N of this wave's vector-memory operations are outstanding; no access to
-// memory moves across.
-template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory"); }
+// memory moves across.  (The builtin, so that the compiler knows its own loads done.)
+template <int N> __device__ __forceinline__ void wait_loads() {
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+    asm volatile("" : : : "memory");
+}
 // Waits until this wave's reads of LDS are done.
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory"); }
 
@@ -286,6 +289,7 @@ struct States {
     int share;   // batch entries that read one problem: 1, or B
     int causal;  // query t reads rows [0, len - T + 1 + t) only
     int rows;    // share G T
+    int rw;      // 32 rw rows to a workgroup of 8 waves; 0: 32 rows to one of 4
     int tiles;   // row tiles of a problem
     int splits;  // pieces of the states' rows
     int slot;    // first partial result of these states

@@ -26,12 +26,13 @@ template <typename S, int D> struct DqRows {
     float lse2, delta;
 };
 
+// s = q k and u = dO v of 32 staged rows of the states.
 template <typename S, int D>
-__device__ __forceinline__ void dq_step(const char *__restrict kt, const char *__restrict vt, int row0, int base,
-                                        int len, float scale, DqRows<S, D> &w) {
+__device__ __forceinline__ void dq_products(const char *kt, const char *vt, int row0, f32x16_t &s, f32x16_t &u,
+                                            const DqRows<S, D> &w) {
     typedef Tile<S, D> X;
     const int lane = threadIdx.x & 63, h = lane >> 5;
-    f32x16_t s = zero16(), u = zero16();
+    s = u = zero16();
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
         Frag<S> f;
@@ -44,6 +45,12 @@ __device__ __forceinline__ void dq_step(const char *__restrict kt, const char *_
         X::row_frag(vt, row0 + (lane & 31), ks, h, f);
         u = mma(f, w.g[ks], u);
     }
+}
+// dq += dS k over them; their first is row `base` of len.
+template <typename S, int D>
+__device__ __forceinline__ void dq_add(const char *kt, int row0, int base, int len, float scale, f32x16_t &s,
+                                       const f32x16_t &u, DqRows<S, D> &w) {
+    const int h = (threadIdx.x >> 5) & 1;
     if (base + 32 > len) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -57,14 +64,149 @@ __device__ __forceinline__ void dq_step(const char *__restrict kt, const char *_
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) {
             Frag<S> f;
-            X::operand_t(kt, row0 + 16 * a, dt, f);
+            Tile<S, D>::operand_t(kt, row0 + 16 * a, dt, f);
             w.acc[dt] = p.add(f, w.acc[dt]);
         }
     }
 }
 
+// 32 rows of the states of a wave, and their gradients.
+template <typename S, int D> struct KvRows {
+    Frag<S> k[D / 16], v[D / 16];
+    f32x16_t dk[D / 32], dv[D / 32];
+};
+
+// The weights p (in s) and dS (in u) of a staged tile of queries: q, dO, statistics.
+template <typename S, int D>
+__device__ __forceinline__ void kv_products(const char *qt, float scale, f32x16_t &s, f32x16_t &u,
+                                            const KvRows<S, D> &w) {
+    typedef Tile<S, D> X;
+    const int lane = threadIdx.x & 63, h = lane >> 5;
+    const char *gt = qt + 32 * X::kRow;
+    const float *st = (const float *)(gt + 32 * X::kRow);
+    s = u = zero16();
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        Frag<S> f;
+        X::row_frag(qt, lane & 31, ks, h, f);
+        s = mma(f, w.k[ks], s);
+    }
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+        Frag<S> f;
+        X::row_frag(gt, lane & 31, ks, h, f);
+        u = mma(f, w.v[ks], u);
+    }
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const f32x4_t lse2 = *reinterpret_cast<const f32x4_t *>(st + 8 * x + 4 * h);
+        const f32x4_t delta = *reinterpret_cast<const f32x4_t *>(st + 32 + 8 * x + 4 * h);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+            const float p = ex2(fmaf(s[4 * x + y], scale, -lse2[y]));
+            s[4 * x + y] = p;
+            u[4 * x + y] = p * (u[4 * x + y] - delta[y]);
+        }
+    }
+}
+template <typename S, int D>
+__device__ __forceinline__ void kv_add_v(const char *qt, const f32x16_t &p, KvRows<S, D> &w) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const Weights<S> pw(p, x);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) {
+            Frag<S> f;
+            Tile<S, D>::operand_t(qt + 32 * Tile<S, D>::kRow, 16 * x, dt, f);
+            w.dv[dt] = pw.add(f, w.dv[dt]);
+        }
+    }
+}
+template <typename S, int D>
+__device__ __forceinline__ void kv_add_k(const char *qt, const f32x16_t &ds, KvRows<S, D> &w) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        const Weights<S> dw(ds, x);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) {
+            Frag<S> f;
+            Tile<S, D>::operand_t(qt, 16 * x, dt, f);
+            w.dk[dt] = dw.add(f, w.dk[dt]);
+        }
+    }
+}
+
+// One item of the dq kernels: its problem, its rows and its piece of the states.
+template <typename S, int D> struct DqItem {
+    int b0, j, piece, len;
+    const char *kp, *vp;
+    long long ks, vs;
+    int b, hh, t;  // the lane's row
+    long long id;
+    bool on;
+
+    __device__ __forceinline__ DqItem(const Gradients &a, int prob, int row0, int piece_) {
+        b0 = prob / a.Hkv;
+        j = prob % a.Hkv;
+        piece = piece_;
+        len = a.lens ? min(max(a.lens[b0], 0), a.S) : a.S;
+        kp = (const char *)((const S *)a.k + b0 * a.lk.sb + j * a.lk.sh);
+        vp = (const char *)((const S *)a.v + b0 * a.lv.sb + j * a.lv.sh);
+        ks = a.lk.st * (long long)sizeof(S);
+        vs = a.lv.st * (long long)sizeof(S);
+        const int r = row0 + (int)(threadIdx.x & 31), rc = min(r, a.rows - 1), hq = rc / a.T, bb = hq / a.G;
+        on = r < a.rows;
+        b = b0 + bb;
+        hh = j * a.G + (hq - bb * a.G);
+        t = rc - hq * a.T;
+        id = ((long long)b * a.H + hh) * a.T + t;
+    }
+    // The rows' q, dO, lse and D; the first piece leaves lse log2 e and D for dk and dv.
+    __device__ __forceinline__ void load(const Gradients &a, bool leave, DqRows<S, D> &w) const {
+        const int h = (threadIdx.x >> 5) & 1;
+        const S *q = (const S *)a.q + b * a.lq.sb + hh * a.lq.sh + t * a.lq.st;
+        const S *g = (const S *)a.g + b * a.lg.sb + hh * a.lg.sh + t * a.lg.st;
+        const S *o = (const S *)a.o + b * a.lo.sb + hh * a.lo.sh + t * a.lo.st;
+        float delta = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+            Frag<S> f;
+            load_frag(q, ks, h, w.q[ks]);
+            load_frag(g, ks, h, w.g[ks]);
+            load_frag(o, ks, h, f);
+            delta += dot_frag(w.g[ks], f);
+        }
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt) w.acc[dt] = zero16();
+        const float lse = a.lse[id];
+        // a row that read nothing has weights of 0
+        w.lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
+        w.delta = half_sum(delta);
+        if (leave && on && h == 0) {
+            float *st = a.stats + stat_at(a, b, hh, t);
+            st[0] = w.lse2;
+            st[32] = w.delta;
+            // positions behind the last one of the head count nothing
+            if (t == a.T - 1)
+                for (int e = t + 1; e & 31; ++e) {
+                    float *x = a.stats + stat_at(a, b, hh, e);
+                    x[0] = INFINITY;
+                    x[32] = 0.f;
+                }
+        }
+    }
+    // Columns 32 dt .. of the lane's row of dq, or of its piece.
+    template <int N> __device__ __forceinline__ void store(const Gradients &a, int d, const f32x16_t *acc) const {
+        const int h = (threadIdx.x >> 5) & 1;
+        if (!on) return;
+        if (a.dq_pieces > 1)
+            store_cols<N>(a.dq_part + (piece * ((long long)a.B * a.H * a.T) + id) * D + d, acc, a.tau, h);
+        else
+            store_cols<N>((S *)a.dq + b * a.ldq.sb + hh * a.ldq.sh + t * a.ldq.st + d, acc, a.tau, h);
+    }
+};
+
 // 128 query rows a workgroup, 32 to a wave; the rows of the states are staged for all four.
-// The first piece also leaves lse log2 e and D of its rows for dk and dv.
 template <typename S, int D>
 __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross_dq_kernel(Gradients a, int items) {
     typedef Tile<S, D> X;
@@ -73,61 +215,24 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
     const int blk = blockIdx.y * gridDim.x + blockIdx.x;
     if (blk >= items) return;
     const int item = xcd_item(blk, items);
-    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const int tile = item % a.row_tiles, piece = item / a.row_tiles % a.dq_pieces,
-              prob = item / a.row_tiles / a.dq_pieces;
-    const int b0 = prob / a.Hkv, j = prob % a.Hkv;
-    const int len = a.lens ? min(max(a.lens[b0], 0), a.S) : a.S;
-    const int r0 = 128 * tile + 32 * wv, r = r0 + (lane & 31);
-    const bool on = r < a.rows, idle = r0 >= a.rows;
-    const int rc = min(r, a.rows - 1), hq = rc / a.T, bb = hq / a.G;
-    const int b = b0 + bb, hh = j * a.G + (hq - bb * a.G), t = rc - hq * a.T;
-    const long long id = ((long long)b * a.H + hh) * a.T + t;
-
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = item % a.row_tiles, piece = item / a.row_tiles % a.dq_pieces;
+    const DqItem<S, D> x(a, item / a.row_tiles / a.dq_pieces, 128 * tile + 32 * wv, piece);
+    const bool idle = 128 * tile + 32 * wv >= a.rows;
+    const int len = x.len;
     DqRows<S, D> w;
-    const S *q = (const S *)a.q + b * a.lq.sb + hh * a.lq.sh + t * a.lq.st;
-    const S *g = (const S *)a.g + b * a.lg.sb + hh * a.lg.sh + t * a.lg.st;
-    const S *o = (const S *)a.o + b * a.lo.sb + hh * a.lo.sh + t * a.lo.st;
-    float delta = 0.f;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-        Frag<S> f;
-        load_frag(q, ks, h, w.q[ks]);
-        load_frag(g, ks, h, w.g[ks]);
-        load_frag(o, ks, h, f);
-        delta += dot_frag(w.g[ks], f);
-    }
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) w.acc[dt] = zero16();
-    const float lse = a.lse[id];
-    // a row that read nothing has weights of 0
-    w.lse2 = lse == -INFINITY ? INFINITY : lse * kLog2e;
-    w.delta = half_sum(delta);
-    if (piece == 0 && on && h == 0) {
-        float *st = a.stats + stat_at(a, b, hh, t);
-        st[0] = w.lse2;
-        st[32] = w.delta;
-        // positions behind the last one of the head count nothing
-        if (t == a.T - 1)
-            for (int e = t + 1; e & 31; ++e) {
-                float *x = a.stats + stat_at(a, b, hh, e);
-                x[0] = INFINITY;
-                x[32] = 0.f;
-            }
-    }
 
     const int n = (len + NT - 1) / NT;
     const int n0 = (int)((long long)n * piece / a.dq_pieces), n1 = (int)((long long)n * (piece + 1) / a.dq_pieces);
-    const char *kp = (const char *)((const S *)a.k + b0 * a.lk.sb + j * a.lk.sh);
-    const char *vp = (const char *)((const S *)a.v + b0 * a.lv.sb + j * a.lv.sh);
-    const long long ks = a.lk.st * (long long)sizeof(S), vs = a.lv.st * (long long)sizeof(S);
     auto fetch = [&](int i) {
         const int row = i * NT;
         char *dst = lds + ((i - n0) & 1) * 2 * TB;
-        X::template stage<NT, 4>(dst, kp + row * ks, ks, len - row, wv);
-        X::template stage<NT, 4>(dst + TB, vp + row * vs, vs, len - row, wv);
+        X::template stage<NT, 4>(dst, x.kp + row * x.ks, x.ks, len - row, wv);
+        X::template stage<NT, 4>(dst + TB, x.vp + row * x.vs, x.vs, len - row, wv);
     };
     if (n0 < n1) fetch(n0);
+    x.load(a, piece == 0, w);
+    wait_loads<0>();  // the queries too: no wait for them stays in the loop
     for (int i = n0; i < n1; ++i) {
         wait_loads<0>();
         __syncthreads();  // this stage has arrived, the one before has been read
@@ -136,134 +241,234 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
         const char *kt = lds + ((i - n0) & 1) * 2 * TB;
 #pragma unroll
         for (int e = 0; e < NT / 32; ++e)
-            if (i * NT + 32 * e < len) dq_step<S, D>(kt, kt + TB, 32 * e, i * NT + 32 * e, len, a.scale, w);
+            if (i * NT + 32 * e < len) {
+                f32x16_t s, u;
+                dq_products<S, D>(kt, kt + TB, 32 * e, s, u, w);
+                dq_add<S, D>(kt, 32 * e, i * NT + 32 * e, len, a.scale, s, u, w);
+            }
     }
-    if (!on) return;
-    if (a.dq_pieces > 1) {
-        const long long rows = (long long)a.B * a.H * a.T;
-        store_cols<D>(a.dq_part + (piece * rows + id) * D, w.acc, a.tau, h);
-    } else {
-        store_cols<D>((S *)a.dq + b * a.ldq.sb + hh * a.ldq.sh + t * a.ldq.st, w.acc, a.tau, h);
+    x.template store<D>(a, 0, w.acc);
+}
+
+// The four waves' results of the same columns, added in the order of the waves: wave w hands
+// tiles w, w + 4, .. to `put`.  `lds` holds 4 KB to a wave and tile.
+template <int N, typename Put>
+__device__ __forceinline__ void add_waves(const f32x16_t *acc, char *lds, int wv, Put put) {
+    const int lane = threadIdx.x & 63;
+    float *x = (float *)lds;
+    __syncthreads();
+#pragma unroll
+    for (int dt = 0; dt < N; ++dt)
+#pragma unroll
+        for (int e = 0; e < 16; e += 4)
+            *reinterpret_cast<f32x4_t *>(x + ((wv * N + dt) * 4 + e / 4) * 256 + 4 * lane) =
+                f32x4_t{acc[dt][e], acc[dt][e + 1], acc[dt][e + 2], acc[dt][e + 3]};
+    __syncthreads();
+    for (int dt = wv; dt < N; dt += 4) {
+        f32x16_t sum = zero16();
+#pragma unroll
+        for (int o = 0; o < 4; ++o)
+#pragma unroll
+            for (int e = 0; e < 16; e += 4) {
+                const f32x4_t y = *reinterpret_cast<const f32x4_t *>(x + ((o * N + dt) * 4 + e / 4) * 256 + 4 * lane);
+#pragma unroll
+                for (int z = 0; z < 4; ++z) sum[e + z] += y[z];
+            }
+        put(dt, sum);
     }
 }
 
-// 128 rows of the states a workgroup, 32 to a wave with their k and v in registers; tiles of
-// 32 queries of one head (q, dO and their lse, D) are staged for all four, two at a time.
+// 32 query rows for all four waves, each on its own rows of the states (tiles of 32, one in
+// four), staged for the wave alone: for problems too few to fill the CUs by 128 rows.
 template <typename S, int D>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dkdv_kernel(Gradients a, int items) {
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dq_narrow_kernel(Gradients a, int items) {
     typedef Tile<S, D> X;
-    constexpr int QT = kStage<S> / 32, TB = 32 * X::kRow, SB = 2 * TB + 256;  // q, dO, statistics
-    __shared__ __attribute__((aligned(16))) char lds[2 * QT * SB];
+    constexpr int TB = 32 * X::kRow, OPS = 32 / X::kRowsPerLoad, N = D / 32;
+    __shared__ __attribute__((aligned(16))) char lds[8 * TB > 16384 * N ? 8 * TB : 16384 * N];
     const int blk = blockIdx.y * gridDim.x + blockIdx.x;
     if (blk >= items) return;
     const int item = xcd_item(blk, items);
-    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
-    const int tile = item % a.key_tiles, piece = item / a.key_tiles % a.dkv_pieces,
-              prob = item / a.key_tiles / a.dkv_pieces;
-    const int b0 = prob / a.Hkv, j = prob % a.Hkv;
-    const int len = a.lens ? min(max(a.lens[b0], 0), a.S) : a.S;
-    const int c0 = 128 * tile + 32 * wv, c = c0 + (lane & 31);
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = item % a.row_tiles, piece = item / a.row_tiles % a.dq_pieces;
+    const DqItem<S, D> x(a, item / a.row_tiles / a.dq_pieces, 32 * tile, piece);
+    const int len = x.len;
+    DqRows<S, D> w;
 
-    f32x16_t dk[D / 32], dv[D / 32];
-#pragma unroll
-    for (int dt = 0; dt < D / 32; ++dt) dk[dt] = dv[dt] = zero16();
-    if (128 * tile < len) {
-        Frag<S> kf[D / 16], vf[D / 16];
-        const int cc = min(c, len - 1);
+    const int n = (len + 31) / 32;
+    const int n0 = (int)((long long)n * piece / a.dq_pieces), n1 = (int)((long long)n * (piece + 1) / a.dq_pieces);
+    char *kt = lds + 2 * TB * wv, *vt = kt + TB;
+    auto fetch_k = [&](int i) { X::template stage<32, 1>(kt, x.kp + 32 * i * x.ks, x.ks, len - 32 * i, 0); };
+    auto fetch_v = [&](int i) { X::template stage<32, 1>(vt, x.vp + 32 * i * x.vs, x.vs, len - 32 * i, 0); };
+    int i = n0 + wv;
+    if (i < n1) {
+        fetch_v(i);
+        fetch_k(i);
+    }
+    x.load(a, piece == 0 && wv == 0, w);
+    wait_loads<0>();  // the queries too: no wait for them stays in the loop
+    for (; i < n1; i += 4) {
+        wait_loads<0>();
+        f32x16_t s, u;
+        dq_products<S, D>(kt, vt, 0, s, u, w);
+        wait_lds();  // V has been read
+        if (i + 4 < n1) fetch_v(i + 4);
+        dq_add<S, D>(kt, 0, 32 * i, len, a.scale, s, u, w);
+        wait_lds();  // K has been read
+        if (i + 4 < n1) fetch_k(i + 4);
+    }
+    add_waves<N>(w.acc, lds, wv, [&](int dt, const f32x16_t &sum) { x.template store<32>(a, 32 * dt, &sum); });
+}
+
+// One item of the dk, dv kernels: its problem, its piece of the queries, the lane's row of the
+// states.
+template <typename S, int D> struct KvItem {
+    int b0, j, prob, piece, len, c, tiles, n0, n1;
+    __device__ __forceinline__ KvItem(const Gradients &a, int prob_, int row0, int piece_) {
+        prob = prob_;
+        piece = piece_;
+        b0 = prob / a.Hkv;
+        j = prob % a.Hkv;
+        len = a.lens ? min(max(a.lens[b0], 0), a.S) : a.S;
+        c = row0 + (int)(threadIdx.x & 31);
+        tiles = (a.T + 31) / 32;  // of a query head
+        const int n = tiles * a.G * a.share;
+        n0 = (int)((long long)n * piece / a.dkv_pieces);
+        n1 = (int)((long long)n * (piece + 1) / a.dkv_pieces);
+    }
+    __device__ __forceinline__ void load(const Gradients &a, KvRows<S, D> &w) const {
+        const int h = (threadIdx.x >> 5) & 1, cc = min(c, len - 1);
         const S *k = (const S *)a.k + b0 * a.lk.sb + j * a.lk.sh + cc * a.lk.st;
         const S *v = (const S *)a.v + b0 * a.lv.sb + j * a.lv.sh + cc * a.lv.st;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
-            load_frag(k, ks, h, kf[ks]);
-            load_frag(v, ks, h, vf[ks]);
+            load_frag(k, ks, h, w.k[ks]);
+            load_frag(v, ks, h, w.v[ks]);
         }
-        const int tiles = (a.T + 31) / 32;  // of a head
-        const int n = tiles * a.G * a.share;
-        const int n0 = (int)((long long)n * piece / a.dkv_pieces),
-                  n1 = (int)((long long)n * (piece + 1) / a.dkv_pieces);
-        const long long qs = a.lq.st * (long long)sizeof(S), gs = a.lg.st * (long long)sizeof(S);
-        auto fetch = [&](int i, int slot) {
-            const int hq = i / tiles, t0 = (i - hq * tiles) * 32, bb = hq / a.G;
-            const int b = b0 + bb, hh = j * a.G + (hq - bb * a.G);
-            char *dst = lds + slot * SB;
-            X::template stage<32, 4>(dst, (const char *)((const S *)a.q + b * a.lq.sb + hh * a.lq.sh + t0 * a.lq.st),
-                                     qs, a.T - t0, wv);
-            X::template stage<32, 4>(dst + TB,
-                                     (const char *)((const S *)a.g + b * a.lg.sb + hh * a.lg.sh + t0 * a.lg.st), gs,
-                                     a.T - t0, wv);
-            if (wv == 3)
-                load_lds4(uniform(lds_address(dst + 2 * TB)), buffer_of(a.stats + stat_at(a, b, hh, t0), 256), 4 * lane);
-        };
-        auto fetch_all = [&](int i, int half) {
+    }
+    // Queries 32 i .. (q, dO and their statistics) to a stage, by NW waves of which this is w.
+    // The statistics go last, by the last wave.
+    template <int NW> __device__ __forceinline__ void fetch_g(const Gradients &a, int i, char *dst, int w) const {
+        typedef Tile<S, D> X;
+        const int hq = i / tiles, t0 = (i - hq * tiles) * 32, bb = hq / a.G, b = b0 + bb, hh = j * a.G + (hq - bb * a.G);
+        X::template stage<32, NW>(dst + 32 * X::kRow,
+                                  (const char *)((const S *)a.g + b * a.lg.sb + hh * a.lg.sh + t0 * a.lg.st),
+                                  a.lg.st * (long long)sizeof(S), a.T - t0, w);
+    }
+    template <int NW> __device__ __forceinline__ void fetch_q(const Gradients &a, int i, char *dst, int w) const {
+        typedef Tile<S, D> X;
+        const int hq = i / tiles, t0 = (i - hq * tiles) * 32, bb = hq / a.G, b = b0 + bb, hh = j * a.G + (hq - bb * a.G);
+        X::template stage<32, NW>(dst, (const char *)((const S *)a.q + b * a.lq.sb + hh * a.lq.sh + t0 * a.lq.st),
+                                  a.lq.st * (long long)sizeof(S), a.T - t0, w);
+        if (w == NW - 1)
+            load_lds4(uniform(lds_address(dst + 64 * X::kRow)), buffer_of(a.stats + stat_at(a, b, hh, t0), 256),
+                      4 * (int)(threadIdx.x & 63));
+    }
+    // Columns d .. d + N - 1 of the lane's row of dk (which 0) or dv (1), or of its piece.
+    template <int N>
+    __device__ __forceinline__ void store(const Gradients &a, int which, int d, const f32x16_t *acc, float scale) const {
+        const int h = (threadIdx.x >> 5) & 1;
+        if (c >= a.S) return;
+        const f32x16_t none[N / 32] = {};
+        const f32x16_t *x = c < len ? acc : none;  // 0 for rows that no query reads
+        if (a.dkv_pieces > 1) {
+            const long long row = piece * ((long long)a.Bkv * a.Hkv * a.S) + (long long)prob * a.S + c;
+            store_cols<N>((which ? a.dv_part : a.dk_part) + row * D + d, x, scale, h);
+        } else {
+            const Layout &l = which ? a.ldv : a.ldk;
+            store_cols<N>((S *)(which ? a.dv : a.dk) + b0 * l.sb + j * l.sh + c * l.st + d, x, scale, h);
+        }
+    }
+};
+
+// 128 rows of the states a workgroup, 32 to a wave with their k and v in registers; tiles of
+// 32 queries of one head (q, dO and their statistics) are staged for all four, two at a time.
+template <typename S, int D>
+__global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross_dkdv_kernel(Gradients a, int items) {
+    constexpr int QT = kStage<S> / 32, SB = 64 * Tile<S, D>::kRow + 256;
+    __shared__ __attribute__((aligned(16))) char lds[2 * QT * SB];
+    const int blk = blockIdx.y * gridDim.x + blockIdx.x;
+    if (blk >= items) return;
+    const int item = xcd_item(blk, items);
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = item % a.key_tiles, piece = item / a.key_tiles % a.dkv_pieces;
+    const KvItem<S, D> x(a, item / a.key_tiles / a.dkv_pieces, 128 * tile + 32 * wv, piece);
+    const bool idle = 128 * tile + 32 * wv >= x.len;
+    KvRows<S, D> w;
+#pragma unroll
+    for (int dt = 0; dt < D / 32; ++dt) w.dk[dt] = w.dv[dt] = zero16();
+    if (128 * tile < x.len) {
+        auto fetch = [&](int i, int half) {
 #pragma unroll
             for (int e = 0; e < QT; ++e)
-                if (i + e < n1) fetch(i + e, half * QT + e);
+                if (i + e < x.n1) {
+                    char *dst = lds + (half * QT + e) * SB;
+                    x.template fetch_g<4>(a, i + e, dst, wv);
+                    x.template fetch_q<4>(a, i + e, dst, wv);
+                }
         };
-        if (n0 < n1) fetch_all(n0, 0);
+        if (x.n0 < x.n1) fetch(x.n0, 0);
+        x.load(a, w);
+        wait_loads<0>();  // k and v too: no wait for them stays in the loop
         int half = 0;
-        for (int i = n0; i < n1; i += QT, half ^= 1) {
+        for (int i = x.n0; i < x.n1; i += QT, half ^= 1) {
             wait_loads<0>();
             __syncthreads();  // this stage has arrived, the one before has been read
-            if (i + QT < n1) fetch_all(i + QT, half ^ 1);
-            if (c0 >= len) continue;
+            if (i + QT < x.n1) fetch(i + QT, half ^ 1);
+            if (idle) continue;
 #pragma unroll
             for (int e = 0; e < QT; ++e) {
-                if (i + e >= n1) break;
-                const char *qt = lds + (half * QT + e) * SB, *gt = qt + TB;
-                const float *st = (const float *)(qt + 2 * TB);
-                f32x16_t s = zero16(), u = zero16();
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    Frag<S> f;
-                    X::row_frag(qt, lane & 31, ks, h, f);
-                    s = mma(f, kf[ks], s);
-                }
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks) {
-                    Frag<S> f;
-                    X::row_frag(gt, lane & 31, ks, h, f);
-                    u = mma(f, vf[ks], u);
-                }
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    const f32x4_t lse2 = *reinterpret_cast<const f32x4_t *>(st + 8 * x + 4 * h);
-                    const f32x4_t delta = *reinterpret_cast<const f32x4_t *>(st + 32 + 8 * x + 4 * h);
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const float p = ex2(fmaf(s[4 * x + y], a.scale, -lse2[y]));
-                        s[4 * x + y] = p;
-                        u[4 * x + y] = p * (u[4 * x + y] - delta[y]);
-                    }
-                }
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const Weights<S> p(s, x), ds(u, x);
-#pragma unroll
-                    for (int dt = 0; dt < D / 32; ++dt) {
-                        Frag<S> f;
-                        X::operand_t(gt, 16 * x, dt, f);
-                        dv[dt] = p.add(f, dv[dt]);
-                        X::operand_t(qt, 16 * x, dt, f);
-                        dk[dt] = ds.add(f, dk[dt]);
-                    }
-                }
+                if (i + e >= x.n1) break;
+                const char *qt = lds + (half * QT + e) * SB;
+                f32x16_t s, u;
+                kv_products<S, D>(qt, a.scale, s, u, w);
+                kv_add_v<S, D>(qt, s, w);
+                kv_add_k<S, D>(qt, u, w);
             }
         }
     }
-    if (c >= a.S) return;
-    if (c >= len) {  // rows that no query reads
+    x.template store<D>(a, 0, 0, w.dk, a.tau);
+    x.template store<D>(a, 1, 0, w.dv, 1.f);
+}
+
+// 32 rows of the states for all four waves, each on its own tiles of queries, staged for the
+// wave alone: for problems too few to fill the CUs by 128 rows.
+template <typename S, int D>
+__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dkdv_narrow_kernel(Gradients a, int items) {
+    typedef Tile<S, D> X;
+    constexpr int N = D / 32, SB = 64 * X::kRow + 256;
+    __shared__ __attribute__((aligned(16))) char lds[4 * SB > 16384 * N ? 4 * SB : 16384 * N];
+    const int blk = blockIdx.y * gridDim.x + blockIdx.x;
+    if (blk >= items) return;
+    const int item = xcd_item(blk, items);
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tile = item % a.key_tiles, piece = item / a.key_tiles % a.dkv_pieces;
+    const KvItem<S, D> x(a, item / a.key_tiles / a.dkv_pieces, 32 * tile, piece);
+    KvRows<S, D> w;
 #pragma unroll
-        for (int dt = 0; dt < D / 32; ++dt) dk[dt] = dv[dt] = zero16();
+    for (int dt = 0; dt < N; ++dt) w.dk[dt] = w.dv[dt] = zero16();
+    if (32 * tile < x.len) {
+        char *qt = lds + SB * wv;
+        int i = x.n0 + wv;
+        if (i < x.n1) {
+            x.template fetch_g<1>(a, i, qt, 0);
+            x.template fetch_q<1>(a, i, qt, 0);
+        }
+        x.load(a, w);
+        wait_loads<0>();  // k and v too: no wait for them stays in the loop
+        for (; i < x.n1; i += 4) {
+            wait_loads<0>();
+            f32x16_t s, u;
+            kv_products<S, D>(qt, a.scale, s, u, w);
+            kv_add_v<S, D>(qt, s, w);
+            wait_lds();  // dO has been read
+            if (i + 4 < x.n1) x.template fetch_g<1>(a, i + 4, qt, 0);
+            kv_add_k<S, D>(qt, u, w);
+            wait_lds();  // q has been read
+            if (i + 4 < x.n1) x.template fetch_q<1>(a, i + 4, qt, 0);
+        }
     }
-    if (a.dkv_pieces > 1) {
-        if (c >= len) return;  // the sum over the pieces writes those zeros
-        const long long rows = (long long)a.Bkv * a.Hkv * a.S, id = (long long)prob * a.S + c;
-        store_cols<D>(a.dk_part + (piece * rows + id) * D, dk, a.tau, h);
-        store_cols<D>(a.dv_part + (piece * rows + id) * D, dv, 1.f, h);
-    } else {
-        store_cols<D>((S *)a.dk + b0 * a.ldk.sb + j * a.ldk.sh + c * a.ldk.st, dk, a.tau, h);
-        store_cols<D>((S *)a.dv + b0 * a.ldv.sb + j * a.ldv.sh + c * a.ldv.st, dv, 1.f, h);
-    }
+    add_waves<N>(w.dk, lds, wv, [&](int dt, const f32x16_t &sum) { x.template store<32>(a, 0, 32 * dt, &sum, a.tau); });
+    add_waves<N>(w.dv, lds, wv, [&](int dt, const f32x16_t &sum) { x.template store<32>(a, 1, 32 * dt, &sum, 1.f); });
 }
 
 // Sums the pieces of up to three gradients, in the order of the pieces.
@@ -299,9 +504,11 @@ template <typename S, int D> hipError_t backward(Gradients a, hipStream_t st) {
     const int prob = a.Bkv * a.Hkv;
     const long long n = (long long)prob * a.row_tiles * a.dq_pieces, m = (long long)prob * a.key_tiles * a.dkv_pieces;
     if (n >= 1ll << 31 || m >= 1ll << 31) return hipErrorInvalidValue;
-    hipError_t e = launch(kCrossBwdDq, cross_dq_kernel<S, D>, grid_of(n), dim3(256), 0, st, a, (int)n);
+    hipError_t e = launch(kCrossBwdDq, a.dq_narrow ? cross_dq_narrow_kernel<S, D> : cross_dq_kernel<S, D>, grid_of(n),
+                          dim3(256), 0, st, a, (int)n);
     if (e != hipSuccess) return e;
-    e = launch(kCrossBwdDkDv, cross_dkdv_kernel<S, D>, grid_of(m), dim3(256), 0, st, a, (int)m);
+    e = launch(kCrossBwdDkDv, a.dkv_narrow ? cross_dkdv_narrow_kernel<S, D> : cross_dkdv_kernel<S, D>, grid_of(m),
+               dim3(256), 0, st, a, (int)m);
     if (e != hipSuccess) return e;
     SumJobs jobs{};
     int count = 0;
@@ -330,21 +537,23 @@ template <typename S> hipError_t backward_d(int D, const Gradients &a, hipStream
     }
 }
 
-// Pieces of a sum: enough for two workgroups to a CU, `least` rows or more to each.
-int pieces(long long wgs, long long steps, int least) {
-    const long long want = (512 + wgs - 1) / wgs, most = (steps + least - 1) / least;
+// Workgroups of 128 rows or, where those are fewer than the CUs, narrow ones of 32; and in
+// how many pieces they take the other side's `steps` rows.
+constexpr int kFew = 256, kLeast = 256;
+void divide(long long prob, int rows, int steps, int *narrow, int *tiles, int *pieces) {
+    *narrow = prob * ((rows + 127) / 128) < kFew;
+    *tiles = (rows + (*narrow ? 31 : 127)) / (*narrow ? 32 : 128);
+    const long long wgs = prob * *tiles, want = (256 + wgs - 1) / wgs, most = (steps + kLeast - 1) / kLeast;
     const long long n = want < most ? want : most;
-    return (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+    *pieces = (int)(n < 1 ? 1 : n > 64 ? 64 : n);
 }
 
 }  // namespace
 
 void plan_cross_backward(Gradients *a) {
     const long long prob = (long long)a->Bkv * a->Hkv;
-    a->row_tiles = (a->rows + 127) / 128;
-    a->key_tiles = (a->S + 127) / 128;
-    a->dq_pieces = pieces(prob * a->row_tiles, a->S, 512);
-    a->dkv_pieces = pieces(prob * a->key_tiles, a->rows, 512);
+    divide(prob, a->rows, a->S, &a->dq_narrow, &a->row_tiles, &a->dq_pieces);
+    divide(prob, a->S, a->rows, &a->dkv_narrow, &a->key_tiles, &a->dkv_pieces);
 }
 
 hipError_t launch_cross_backward(int dtype, int D, const Gradients &a, hipStream_t s) {

@@ -8,14 +8,23 @@ namespace fibattn {
 
 namespace {
 
-// Rows of the states a workgroup stages at a time when its waves share them.
-template <typename S> constexpr int kStage = sizeof(S) == 2 ? 64 : 32;
+// A workgroup of 8 waves on 32 RW query rows: RW waves side by side, KW = 8 / RW waves to the
+// same rows, each on its own 32 NS of the staged rows of the states.  Two waves to the same
+// rows double the waves a CU holds (MFMA and exponentials of one wave run beside another's)
+// without a result in memory; more of them serve problems of few rows.
+template <typename S, int D, int RW> struct Shape {
+    static constexpr int KW = 8 / RW;
+    static constexpr int NS = KW == 2 && D * (int)sizeof(S) <= 128 ? 2 : 1;
+    static constexpr int NT = 32 * KW * NS;              // rows of a stage
+    static constexpr int TB = NT * D * (int)sizeof(S);   // bytes of its k, and of its v
+    static constexpr int merge = RW * (KW - 1) * 32 * (D + 2) * 4;
+    static constexpr int lds = 4 * TB > merge ? 4 * TB : merge;
+};
 
-template <typename S, int D> constexpr int lds_bytes() {
-    // shared: K and V, two stages; per wave: K and V of 32 rows
-    constexpr int shared = 2 * 2 * kStage<S> * D * (int)sizeof(S), waves = 4 * 2 * 32 * D * (int)sizeof(S);
-    constexpr int merge = 4 * 32 * D * 4;
-    return shared > waves ? (shared > merge ? shared : merge) : (waves > merge ? waves : merge);
+template <typename S, int D> constexpr int keys_lds() {
+    // per wave: K and V of 32 rows; at the end the waves' results
+    constexpr int waves = 4 * 2 * 32 * D * (int)sizeof(S), merge = 4 * 32 * D * 4;
+    return waves > merge ? waves : merge;
 }
 
 // A wave's 32 query rows.
@@ -133,47 +142,20 @@ struct Redo {
     long long slot;
 };
 
-// One problem's rows of the states; stage i holds rows i NT .. of k, then of v.
-template <typename S, int D> struct Source {
-    const char *k, *v;
-    long long ks, vs;
-    int len;
-    __device__ __forceinline__ void fetch(char *dst, int i, int wv) const {
-        constexpr int NT = kStage<S>;
-        const int r = i * NT;
-        Tile<S, D>::template stage<NT, 4>(dst, k + r * ks, ks, len - r, wv);
-        Tile<S, D>::template stage<NT, 4>(dst + NT * Tile<S, D>::kRow, v + r * vs, vs, len - r, wv);
-    }
-};
-
-// The wave's work on stage i of the states.
-template <typename S, int D>
-__device__ __forceinline__ void rows_step(const char *cur, int i, int low, float scale, Rows<S, D> &w) {
-    constexpr int NT = kStage<S>, NS = NT / 32, TB = NT * Tile<S, D>::kRow;
-    f32x16_t s[NS];
-#pragma unroll
-    for (int e = 0; e < NS; ++e) s[e] = logits<S, D>(cur, 32 * e, w);
-    if ((i + 1) * NT > low) {
-#pragma unroll
-        for (int e = 0; e < NS; ++e) mask<S, D>(s[e], i * NT + 32 * e, w);
-    }
-    weights<S, D, NS>(s, scale, w);
-#pragma unroll
-    for (int e = 0; e < NS; ++e) values<S, D>(cur + TB, 32 * e, s[e], w);
-}
-
-// 128 query rows, 32 to a wave; the waves share the staged rows of the states.
-template <typename S, int D>
+// 32 RW query rows, 32 to a wave; the waves share the staged rows of the states.
+template <typename S, int D, int RW>
 __device__ __forceinline__ void rows_body(const Queries &a, const States &st, int item, char *lds, Redo &todo) {
     typedef Tile<S, D> X;
-    constexpr int NT = kStage<S>, TB = NT * X::kRow;
-    const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    typedef Shape<S, D, RW> Y;
+    constexpr int NT = Y::NT, NS = Y::NS, KW = Y::KW, TB = Y::TB;
+    const int lane = threadIdx.x & 63, h = lane >> 5, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rw = wv % RW, kw = wv / RW;
     const int tile = item % st.tiles, piece = item / st.tiles % st.splits, prob = item / st.tiles / st.splits;
-    const int b0 = prob / a.Hkv, j = prob % a.Hkv;
+    const int b0 = prob / a.Hkv, j = prob % a.Hkv, r0 = 32 * (RW * tile + rw);
     const int len = states_len(st, b0);
     Rows<S, D> w;
-    load_rows<S, D>(a, st, b0, j, 128 * tile + 32 * wv, len, w);
-    const bool idle = 128 * tile + 32 * wv >= st.rows;
+    load_rows<S, D>(a, st, b0, j, r0, len, w);
+    const bool idle = r0 >= st.rows;
 
     const int n = (len + NT - 1) / NT;
     const int n0 = (int)((long long)n * piece / st.splits), n1 = (int)((long long)n * (piece + 1) / st.splits);
@@ -181,16 +163,68 @@ __device__ __forceinline__ void rows_body(const Queries &a, const States &st, in
     const char *kp = (const char *)((const S *)st.k + b0 * st.lk.sb + j * st.lk.sh);
     const char *vp = (const char *)((const S *)st.v + b0 * st.lv.sb + j * st.lv.sh);
     const long long ks = st.lk.st * (long long)sizeof(S), vs = st.lv.st * (long long)sizeof(S);
-    const Source<S, D> src = {kp, vp, ks, vs, len};
-    if (n0 < n1) src.fetch(lds, n0, wv);
+    auto fetch = [&](int i) {
+        const int r = i * NT;
+        char *dst = lds + ((i - n0) & 1) * 2 * TB;
+        X::template stage<NT, 8>(dst, kp + r * ks, ks, len - r, wv);
+        X::template stage<NT, 8>(dst + TB, vp + r * vs, vs, len - r, wv);
+    };
+    if (n0 < n1) fetch(n0);
+    wait_loads<0>();  // the queries too: no wait for them stays in the loop
     for (int i = n0; i < n1; ++i) {
         wait_loads<0>();
         __syncthreads();  // this stage has arrived, the one before has been read
-        const int buf = (i - n0) & 1;
-        if (i + 1 < n1) src.fetch(lds + (buf ^ 1) * 2 * TB, i + 1, wv);
-        if (!idle) rows_step<S, D>(lds + buf * 2 * TB, i, low, a.scale, w);
+        if (i + 1 < n1) fetch(i + 1);
+        const int r = 32 * NS * kw, base = i * NT + r;
+        if (idle || base >= len) continue;
+        const char *kt = lds + ((i - n0) & 1) * 2 * TB, *vt = kt + TB;
+        f32x16_t s[NS];
+#pragma unroll
+        for (int e = 0; e < NS; ++e) s[e] = logits<S, D>(kt, r + 32 * e, w);
+        if (base + 32 * NS > low) {
+#pragma unroll
+            for (int e = 0; e < NS; ++e) mask<S, D>(s[e], base + 32 * e, w);
+        }
+        weights<S, D, NS>(s, a.scale, w);
+#pragma unroll
+        for (int e = 0; e < NS; ++e) values<S, D>(vt, r + 32 * e, s[e], w);
     }
-    const float l = half_sum(w.l), f = l == 0.f ? 0.f : 1.f / l;
+    float l = half_sum(w.l);
+    if (KW > 1) {
+        // the waves of the same rows, joined in their order; lanes hold the same places
+        __syncthreads();
+        float *part = (float *)lds + (rw * (KW - 1)) * 32 * (D + 2);
+        if (kw) {
+            float *x = part + (kw - 1) * 32 * (D + 2);
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4)
+                    *reinterpret_cast<f32x4_t *>(x + (dt * 16 + e) * 64 + 4 * lane) =
+                        f32x4_t{w.acc[dt][e], w.acc[dt][e + 1], w.acc[dt][e + 2], w.acc[dt][e + 3]};
+            x[32 * D + lane] = h ? l : w.m;
+        }
+        __syncthreads();
+        if (kw) return;
+#pragma unroll 1
+        for (int o = 0; o < KW - 1; ++o) {
+            const float *x = part + o * 32 * (D + 2);
+            const float m2 = x[32 * D + (lane & 31)], l2 = x[32 * D + 32 + (lane & 31)], m = fmaxf(w.m, m2);
+            // a wave that met no rows has the maximum -inf: it counts nothing
+            const float f1 = w.m == -INFINITY ? 0.f : ex2(w.m - m), f2 = m2 == -INFINITY ? 0.f : ex2(m2 - m);
+            w.m = m;
+            l = l * f1 + l2 * f2;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+                for (int e = 0; e < 16; e += 4) {
+                    const f32x4_t y = *reinterpret_cast<const f32x4_t *>(x + (dt * 16 + e) * 64 + 4 * lane);
+#pragma unroll
+                    for (int z = 0; z < 4; ++z) w.acc[dt][e + z] = w.acc[dt][e + z] * f1 + y[z] * f2;
+                }
+        }
+    }
+    const float f = l == 0.f ? 0.f : 1.f / l;
     const long long slot = st.slot + piece;
     float nan = 0.f;  // NaN if a value is (or an infinity)
 #pragma unroll
@@ -198,16 +232,15 @@ __device__ __forceinline__ void rows_body(const Queries &a, const States &st, in
 #pragma unroll
         for (int e = 0; e < 16; ++e) nan = fmaf(w.acc[dt][e], 0.f, nan);
     if (__ballot(w.on && nan != 0.f)) {
-        const int r0 = 128 * tile + 32 * wv;
         todo = {b0, j, r0, 1, r0 + 32, n0 * NT, min(n1 * NT, len), len, slot};
         return;
     }
     if (!w.on) return;
-    if (lane < 32) put_lse(a, slot, w.id, w.m, l);
+    if (h == 0) put_lse(a, slot, w.id, w.m, l);
     if (a.part_o)
-        store_cols<D>(a.part_o + (slot * a.B * a.H * a.T + w.id) * D, w.acc, f, lane >> 5);
+        store_cols<D>(a.part_o + (slot * a.B * a.H * a.T + w.id) * D, w.acc, f, h);
     else
-        store_cols<D>(out_row<S, D>(a, w.at), w.acc, f, lane >> 5);
+        store_cols<D>(out_row<S, D>(a, w.at), w.acc, f, h);
 }
 
 // 32 query rows for all four waves, each on its own rows of the states (tiles of 32, one in
@@ -356,47 +389,82 @@ __device__ __forceinline__ void plain_rows(const Queries &a, const States &st, c
     }
 }
 
-// Items of the first states, then of the second (a prefix, then the sequence's own rows).
-template <typename S, int D>
-__global__ __launch_bounds__(256, 2) void cross_fwd_kernel(Queries a, States s0, States s1, int by_keys0, int by_keys1,
-                                                           int n0, int n) {
-    __shared__ __attribute__((aligned(16))) char lds[lds_bytes<S, D>()];
-    const int b = blockIdx.y * gridDim.x + blockIdx.x;
-    if (b >= n) return;
-    const bool first = b < n0;
-    const States st = first ? s0 : s1;
-    const int item = first ? xcd_item(b, n0) : xcd_item(b - n0, n - n0);
+// By rows (RW > 0: 8 waves) or by keys (RW 0: 4 waves).
+template <typename S, int D, int RW> constexpr int waves_of() { return RW ? 8 : 4; }
+
+template <typename S, int D, int RW>
+__device__ __forceinline__ void body(const Queries &a, const States &st, int item, char *lds) {
     Redo todo;
     todo.end = 0;
-    if (first ? by_keys0 : by_keys1)
+    if constexpr (RW == 0)
         keys_body<S, D>(a, st, item, lds, todo);
     else
-        rows_body<S, D>(a, st, item, lds, todo);
+        rows_body<S, D, RW>(a, st, item, lds, todo);
     if (todo.end) plain_rows<S, D>(a, st, todo);
 }
 
+template <typename S, int D, int RW> constexpr int body_lds() {
+    if constexpr (RW == 0)
+        return keys_lds<S, D>();
+    else
+        return Shape<S, D, RW>::lds;
+}
+
+// Waves to a SIMD that the registers are held down for.
+template <typename S, int D, int RW> constexpr int simd_waves() {
+    if (sizeof(S) == 4 && D == 128) return RW ? 2 : 1;
+    return D <= 64 && RW ? 4 : 2;
+}
+
+// Items [0, n0) of s0, then those of s1.
+template <typename S, int D, int RW>
+__global__ __launch_bounds__(RW ? 512 : 256, (simd_waves<S, D, RW>())) void cross_fwd_kernel(Queries a, States s0,
+                                                                                          States s1, int n0, int n) {
+    __shared__ __attribute__((aligned(16))) char lds[body_lds<S, D, RW>()];
+    const int b = blockIdx.y * gridDim.x + blockIdx.x;
+    if (b >= n) return;
+    const bool first = b < n0;
+    body<S, D, RW>(a, first ? s0 : s1, first ? xcd_item(b, n0) : xcd_item(b - n0, n - n0), lds);
+}
+
 // Partial results of a row: o = sum_i exp(lse_i - lse) o_i, lse = log sum_i exp(lse_i).  A
-// part without rows (lse -inf) counts nothing, whatever its o holds.
+// part without rows (lse -inf) counts nothing, whatever its o holds.  A wave to a row: lane i
+// has the weight of part i (at most 64 at a time), and D / 4 lanes add every (256 / D)-th part.
 template <typename S, int D>
 __global__ __launch_bounds__(256) void join_parts_kernel(Queries a, int parts) {
-    constexpr int per = D / 4;
+    constexpr int per = D / 4, groups = 64 / per;
     const long long rows = (long long)a.B * a.H * a.T;
-    const long long e = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
-    const long long r = e / per;
-    const int d = (int)(e % per) * 4;
+    const long long r = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (r >= rows) return;
+    const int lane = threadIdx.x & 63, g = lane / per, d = lane % per * 4;
     float m = -INFINITY;
-    for (int i = 0; i < parts; ++i) m = fmaxf(m, a.part_lse[i * rows + r]);
+    for (int i = lane; i < parts; i += 64) m = fmaxf(m, a.part_lse[i * rows + r]);
+#pragma unroll
+    for (int e = 32; e; e >>= 1) m = fmaxf(m, __shfl_xor(m, e, 64));
     float sum = 0.f;
     f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < parts; ++i) {
-        const float z = a.part_lse[i * rows + r];
-        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(a.part_o + (i * rows + r) * D + d);
-        if (z == -INFINITY) continue;
-        const float f = ex2((z - m) * kLog2e);
+    for (int base = 0; base < parts; base += 64) {
+        const int n = min(64, parts - base);
+        const float z = lane < n ? a.part_lse[(base + lane) * rows + r] : -INFINITY;
+        const float f = z == -INFINITY ? 0.f : ex2((z - m) * kLog2e);
         sum += f;
-        y += x * f;
+        const float *x = a.part_o + ((long long)base * rows + r) * D + d;
+#pragma unroll 4
+        for (int i = g; i < (n + groups - 1) / groups * groups; i += groups) {
+            const float w = __shfl(f, i, 64);
+            f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+            if (i < n) v = *reinterpret_cast<const f32x4_t *>(x + (long long)i * rows * D);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] += w == 0.f ? 0.f : v[e] * w;
+        }
     }
+#pragma unroll
+    for (int e = 32; e; e >>= 1) sum += __shfl_xor(sum, e, 64);
+#pragma unroll
+    for (int e = 32; e >= per; e >>= 1)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) y[c] += __shfl_xor(y[c], e, 64);
+    if (g) return;
     const float f = sum == 0.f ? 0.f : 1.f / sum;
     const int t = (int)(r % a.T), h = (int)(r / a.T % a.H), b = (int)(r / a.T / a.H);
     if (d == 0) a.lse[r] = sum == 0.f ? -INFINITY : m + __log2f(sum) * kLn2;
@@ -430,41 +498,54 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
     if (d == 0) a.z[r] = sum == 0.f ? -INFINITY : m + __log2f(sum) * kLn2;
 }
 
-// Row tiles and pieces of states for `prob` problems.  Few rows (at most 32 to a problem) go
-// to workgroups whose waves take different rows of the states.
-void plan(States *s, int prob, int *by_keys) {
-    *by_keys = s->rows <= 32;
-    s->tiles = (s->rows + (*by_keys ? 31 : 127)) / (*by_keys ? 32 : 128);
+// Rows to a workgroup, row tiles and pieces of states for `prob` problems.  Few rows (at most
+// 32 to a problem) go to workgroups whose waves take different rows of the states.
+constexpr int kByKeys = 512;
+void plan(States *s, int prob) {
+    s->rw = s->rows <= kByKeys ? 0 : 4;
+    const int per = s->rw ? 32 * s->rw : 32;
+    s->tiles = (s->rows + per - 1) / per;
     const long long wgs = (long long)prob * s->tiles;
     // two workgroups to a CU; a piece keeps 256 rows or more
-    const long long want = (512 + wgs - 1) / wgs, most = (s->S + 255) / 256;
+    const long long want = (256 + wgs - 1) / wgs, most = (s->S + 255) / 256;
     s->splits = (int)(want < 1 ? 1 : want < most ? want : most);
     if (s->splits > 64) s->splits = 64;
 }
 
+template <typename S, int D, int RW>
+hipError_t launch_as(const Queries &q, const States &s0, const States &s1, long long n0, long long n, hipStream_t st) {
+    if (n >= 1ll << 31) return hipErrorInvalidValue;
+    return launch(kCrossForward, cross_fwd_kernel<S, D, RW>, grid_of(n, RW ? 512 : 256), dim3(RW ? 512 : 256), 0, st, q,
+                  s0, s1, (int)n0, (int)n);
+}
+template <typename S, int D>
+hipError_t launch_parts(const Queries &q, const States &s0, const States &s1, long long n0, long long n, hipStream_t st) {
+    return s0.rw ? launch_as<S, D, 4>(q, s0, s1, n0, n, st) : launch_as<S, D, 0>(q, s0, s1, n0, n, st);
+}
+
 template <typename S, int D>
 hipError_t forward(const Queries &a, States s0, const States *s1, int prob0, int prob1, hipStream_t st) {
-    int k0, k1 = 0;
-    plan(&s0, prob0, &k0);
-    States second = s0;
-    long long n0 = (long long)prob0 * s0.tiles * s0.splits, n = n0;
+    plan(&s0, prob0);
+    States own = s0;
     int parts = s0.splits;
-    s0.slot = 0;
+    const long long n0 = (long long)prob0 * s0.tiles * s0.splits;
+    long long n1 = 0;
     if (s1) {
-        second = *s1;
-        plan(&second, prob1, &k1);
-        second.slot = parts;
-        parts += second.splits;
-        n += (long long)prob1 * second.tiles * second.splits;
+        own = *s1;
+        plan(&own, prob1);
+        own.slot = parts;
+        parts += own.splits;
+        n1 = (long long)prob1 * own.tiles * own.splits;
     }
-    if (n >= 1ll << 31) return hipErrorInvalidValue;
     Queries q = a;
     if (parts == 1) q.part_o = q.part_lse = nullptr;
-    hipError_t e = launch(kCrossForward, cross_fwd_kernel<S, D>, grid_of(n), dim3(256), 0, st, q, s0, second, k0, k1,
-                          (int)n0, (int)n);
+    // states that are read the same way share a launch
+    const bool both = own.rw == s0.rw;
+    hipError_t e = launch_parts<S, D>(q, s0, own, n0, both ? n0 + n1 : n0, st);
+    if (e == hipSuccess && !both) e = launch_parts<S, D>(q, own, own, n1, n1, st);
     if (e != hipSuccess || parts == 1) return e;
-    const long long threads = (long long)a.B * a.H * a.T * (D / 4);
-    return launch(kJoin, join_parts_kernel<S, D>, grid_of((threads + 255) / 256), dim3(256), 0, st, q, parts);
+    const long long rows = (long long)a.B * a.H * a.T;
+    return launch(kJoin, join_parts_kernel<S, D>, grid_of((rows + 3) / 4), dim3(256), 0, st, q, parts);
 }
 
 template <typename S>
@@ -492,8 +573,7 @@ int cross_forward_parts(int rows, int S, int prob) {
     States s{};
     s.rows = rows;
     s.S = S;
-    int k;
-    plan(&s, prob, &k);
+    plan(&s, prob);
     return s.splits;
 }
 

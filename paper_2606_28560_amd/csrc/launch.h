@@ -33,10 +33,10 @@ hipError_t launch(int id, void (*kernel)(P...), dim3 grid, dim3 block, unsigned 
     return hipGetLastError();
 }
 
-// Grid of `blocks` workgroups of up to 256 threads: one row, or rows of 2^23 (a dimension
-// times the workgroup's threads stays below 2^32); kernels drop the last row's excess.
-inline dim3 grid_of(long long blocks) {
-    const long long x = blocks < (1ll << 23) ? blocks : 1ll << 23;
+// Grid of `blocks` workgroups of up to `threads` threads: one row, or rows of 2^31 threads (a
+// dimension times the workgroup's threads stays below 2^32); kernels drop the last row's excess.
+inline dim3 grid_of(long long blocks, int threads = 256) {
+    const long long row = (1ll << 31) / threads, x = blocks < row ? blocks : row;
     return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
 }
 
