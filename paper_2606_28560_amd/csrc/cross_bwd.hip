@@ -278,13 +278,17 @@ __device__ __forceinline__ void add_waves(const f32x16_t *acc, char *lds, int wv
     }
 }
 
+// Stages of a wave's own: two where a tile's products are shorter than its way from memory
+// (bfloat16), one in float32, whose tiles take eight times the matrix-core time.
+template <typename S> constexpr int kPrivate = sizeof(S) == 2 ? 2 : 1;
+
 // 32 query rows for all four waves, each on its own rows of the states (tiles of 32, one in
 // four), staged for the wave alone: for problems too few to fill the CUs by 128 rows.
 template <typename S, int D>
 __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dq_narrow_kernel(Gradients a, int items) {
     typedef Tile<S, D> X;
-    constexpr int TB = 32 * X::kRow, OPS = 32 / X::kRowsPerLoad, N = D / 32;
-    __shared__ __attribute__((aligned(16))) char lds[8 * TB > 16384 * N ? 8 * TB : 16384 * N];
+    constexpr int NB = kPrivate<S>, TB = 32 * X::kRow, N = D / 32;
+    __shared__ __attribute__((aligned(16))) char lds[8 * NB * TB > 16384 * N ? 8 * NB * TB : 16384 * N];
     const int blk = blockIdx.y * gridDim.x + blockIdx.x;
     if (blk >= items) return;
     const int item = xcd_item(blk, items);
@@ -296,25 +300,38 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dq_narrow_kernel(
 
     const int n = (len + 31) / 32;
     const int n0 = (int)((long long)n * piece / a.dq_pieces), n1 = (int)((long long)n * (piece + 1) / a.dq_pieces);
-    char *kt = lds + 2 * TB * wv, *vt = kt + TB;
-    auto fetch_k = [&](int i) { X::template stage<32, 1>(kt, x.kp + 32 * i * x.ks, x.ks, len - 32 * i, 0); };
-    auto fetch_v = [&](int i) { X::template stage<32, 1>(vt, x.vp + 32 * i * x.vs, x.vs, len - 32 * i, 0); };
-    int i = n0 + wv;
+    char *mine = lds + 2 * NB * TB * wv;
+    auto fetch_k = [&](int i, char *kt) { X::template stage<32, 1>(kt, x.kp + 32 * i * x.ks, x.ks, len - 32 * i, 0); };
+    auto fetch_v = [&](int i, char *kt) {
+        X::template stage<32, 1>(kt + TB, x.vp + 32 * i * x.vs, x.vs, len - 32 * i, 0);
+    };
+    int i = n0 + wv, buf = 0;
     if (i < n1) {
-        fetch_v(i);
-        fetch_k(i);
+        fetch_v(i, mine);
+        fetch_k(i, mine);
     }
     x.load(a, piece == 0 && wv == 0, w);
     wait_loads<0>();  // the queries too: no wait for them stays in the loop
-    for (; i < n1; i += 4) {
+    for (; i < n1; i += 4, buf ^= NB - 1) {
+        const bool more = i + 4 < n1;
+        char *kt = mine + 2 * TB * buf, *next = mine + 2 * TB * (buf ^ (NB - 1));
         wait_loads<0>();
+        wait_lds();
+        if (NB == 2 && more) {
+            fetch_v(i + 4, next);
+            fetch_k(i + 4, next);
+        }
         f32x16_t s, u;
-        dq_products<S, D>(kt, vt, 0, s, u, w);
-        wait_lds();  // V has been read
-        if (i + 4 < n1) fetch_v(i + 4);
+        dq_products<S, D>(kt, kt + TB, 0, s, u, w);
+        if (NB == 1 && more) {
+            wait_lds();  // V has been read
+            fetch_v(i + 4, kt);
+        }
         dq_add<S, D>(kt, 0, 32 * i, len, a.scale, s, u, w);
-        wait_lds();  // K has been read
-        if (i + 4 < n1) fetch_k(i + 4);
+        if (NB == 1 && more) {
+            wait_lds();  // K has been read
+            fetch_k(i + 4, kt);
+        }
     }
     add_waves<N>(w.acc, lds, wv, [&](int dt, const f32x16_t &sum) { x.template store<32>(a, 32 * dt, &sum); });
 }
@@ -345,22 +362,39 @@ template <typename S, int D> struct KvItem {
             load_frag(v, ks, h, w.v[ks]);
         }
     }
-    // Queries 32 i .. (q, dO and their statistics) to a stage, by NW waves of which this is w.
-    // The statistics go last, by the last wave.
-    template <int NW> __device__ __forceinline__ void fetch_g(const Gradients &a, int i, char *dst, int w) const {
-        typedef Tile<S, D> X;
-        const int hq = i / tiles, t0 = (i - hq * tiles) * 32, bb = hq / a.G, b = b0 + bb, hh = j * a.G + (hq - bb * a.G);
-        X::template stage<32, NW>(dst + 32 * X::kRow,
-                                  (const char *)((const S *)a.g + b * a.lg.sb + hh * a.lg.sh + t0 * a.lg.st),
-                                  a.lg.st * (long long)sizeof(S), a.T - t0, w);
+    // A tile of queries: positions 32 tt .. of member g of the group, batch entry b0 + bb.
+    struct At {
+        int tt, g, bb;
+    };
+    __device__ __forceinline__ At tile_at(const Gradients &a, int i) const {
+        const int hq = i / tiles, bb = hq / a.G;
+        return {i - hq * tiles, hq - bb * a.G, bb};
     }
-    template <int NW> __device__ __forceinline__ void fetch_q(const Gradients &a, int i, char *dst, int w) const {
+    __device__ __forceinline__ void step(const Gradients &a, At &at, int by) const {
+        at.tt += by;
+        while (at.tt >= tiles) {
+            at.tt -= tiles;
+            if (++at.g == a.G) {
+                at.g = 0;
+                ++at.bb;
+            }
+        }
+    }
+    // Its dO, and its q and statistics, to a stage (q, dO, statistics) by NW waves of which this
+    // is w.
+    template <int NW> __device__ __forceinline__ void fetch_g(const Gradients &a, const At &at, char *dst, int w) const {
         typedef Tile<S, D> X;
-        const int hq = i / tiles, t0 = (i - hq * tiles) * 32, bb = hq / a.G, b = b0 + bb, hh = j * a.G + (hq - bb * a.G);
-        X::template stage<32, NW>(dst, (const char *)((const S *)a.q + b * a.lq.sb + hh * a.lq.sh + t0 * a.lq.st),
-                                  a.lq.st * (long long)sizeof(S), a.T - t0, w);
+        const S *g = (const S *)a.g + (b0 + at.bb) * a.lg.sb + (j * a.G + at.g) * a.lg.sh + 32 * at.tt * a.lg.st;
+        X::template stage<32, NW>(dst + 32 * X::kRow, (const char *)g, a.lg.st * (long long)sizeof(S), a.T - 32 * at.tt, w);
+    }
+    template <int NW> __device__ __forceinline__ void fetch_q(const Gradients &a, const At &at, char *dst, int w) const {
+        typedef Tile<S, D> X;
+        const int b = b0 + at.bb, hh = j * a.G + at.g;
+        const S *q = (const S *)a.q + b * a.lq.sb + hh * a.lq.sh + 32 * at.tt * a.lq.st;
+        X::template stage<32, NW>(dst, (const char *)q, a.lq.st * (long long)sizeof(S), a.T - 32 * at.tt, w);
         if (w == NW - 1)
-            load_lds4(uniform(lds_address(dst + 64 * X::kRow)), buffer_of(a.stats + stat_at(a, b, hh, t0), 256),
+            load_lds4(uniform(lds_address(dst + 64 * X::kRow)),
+                      buffer_of(a.stats + (((long long)b * a.H + hh) * tiles + at.tt) * 64, 256),
                       4 * (int)(threadIdx.x & 63));
     }
     // Columns d .. d + N - 1 of the lane's row of dk (which 0) or dv (1), or of its piece.
@@ -397,13 +431,15 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) w.dk[dt] = w.dv[dt] = zero16();
     if (128 * tile < x.len) {
+        auto at = x.tile_at(a, x.n0);
         auto fetch = [&](int i, int half) {
 #pragma unroll
             for (int e = 0; e < QT; ++e)
                 if (i + e < x.n1) {
                     char *dst = lds + (half * QT + e) * SB;
-                    x.template fetch_g<4>(a, i + e, dst, wv);
-                    x.template fetch_q<4>(a, i + e, dst, wv);
+                    x.template fetch_g<4>(a, at, dst, wv);
+                    x.template fetch_q<4>(a, at, dst, wv);
+                    x.step(a, at, 1);
                 }
         };
         if (x.n0 < x.n1) fetch(x.n0, 0);
@@ -435,8 +471,8 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
 template <typename S, int D>
 __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dkdv_narrow_kernel(Gradients a, int items) {
     typedef Tile<S, D> X;
-    constexpr int N = D / 32, SB = 64 * X::kRow + 256;
-    __shared__ __attribute__((aligned(16))) char lds[4 * SB > 16384 * N ? 4 * SB : 16384 * N];
+    constexpr int NB = kPrivate<S>, N = D / 32, SB = 64 * X::kRow + 256;
+    __shared__ __attribute__((aligned(16))) char lds[4 * NB * SB > 16384 * N ? 4 * NB * SB : 16384 * N];
     const int blk = blockIdx.y * gridDim.x + blockIdx.x;
     if (blk >= items) return;
     const int item = xcd_item(blk, items);
@@ -447,24 +483,37 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dkdv_narrow_kerne
 #pragma unroll
     for (int dt = 0; dt < N; ++dt) w.dk[dt] = w.dv[dt] = zero16();
     if (32 * tile < x.len) {
-        char *qt = lds + SB * wv;
-        int i = x.n0 + wv;
+        char *mine = lds + NB * SB * wv;
+        int i = x.n0 + wv, buf = 0;
+        auto at = x.tile_at(a, i);  // of the tile that is fetched
         if (i < x.n1) {
-            x.template fetch_g<1>(a, i, qt, 0);
-            x.template fetch_q<1>(a, i, qt, 0);
+            x.template fetch_g<1>(a, at, mine, 0);
+            x.template fetch_q<1>(a, at, mine, 0);
         }
         x.load(a, w);
         wait_loads<0>();  // k and v too: no wait for them stays in the loop
-        for (; i < x.n1; i += 4) {
+        for (; i < x.n1; i += 4, buf ^= NB - 1) {
+            const bool more = i + 4 < x.n1;
+            char *qt = mine + SB * buf, *next = mine + SB * (buf ^ (NB - 1));
             wait_loads<0>();
+            wait_lds();
+            x.step(a, at, 4);
+            if (NB == 2 && more) {
+                x.template fetch_g<1>(a, at, next, 0);
+                x.template fetch_q<1>(a, at, next, 0);
+            }
             f32x16_t s, u;
             kv_products<S, D>(qt, a.scale, s, u, w);
             kv_add_v<S, D>(qt, s, w);
-            wait_lds();  // dO has been read
-            if (i + 4 < x.n1) x.template fetch_g<1>(a, i + 4, qt, 0);
+            if (NB == 1 && more) {
+                wait_lds();  // dO has been read
+                x.template fetch_g<1>(a, at, qt, 0);
+            }
             kv_add_k<S, D>(qt, u, w);
-            wait_lds();  // q has been read
-            if (i + 4 < x.n1) x.template fetch_q<1>(a, i + 4, qt, 0);
+            if (NB == 1 && more) {
+                wait_lds();  // q has been read
+                x.template fetch_q<1>(a, at, qt, 0);
+            }
         }
     }
     add_waves<N>(w.dk, lds, wv, [&](int dt, const f32x16_t &sum) { x.template store<32>(a, 0, 32 * dt, &sum, a.tau); });
