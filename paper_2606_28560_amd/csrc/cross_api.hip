@@ -49,21 +49,21 @@ void place_parts(Queries *a, void *workspace, int parts, int D) {
 }
 
 // Pieces of the forward over a batch's own states (B_kv = B) or shared ones (B_kv = 1).
-int forward_parts(int B, int B_kv, int H, int H_kv, int T, int S) {
-    return cross_forward_parts(B / B_kv * (H / H_kv) * T, S, B_kv * H_kv);
+int forward_parts(int dtype, int D, int B, int B_kv, int H, int H_kv, int T, int S) {
+    return cross_forward_parts(dtype, D, B / B_kv * (H / H_kv) * T, S, B_kv * H_kv);
 }
 
 struct BackwardPlan {
     Gradients g;
     size_t dq, dk, dv, total;  // offsets behind the statistics
 };
-BackwardPlan plan_backward(int B, int B_kv, int H, int H_kv, int T, int S, int D) {
+BackwardPlan plan_backward(int dtype, int B, int B_kv, int H, int H_kv, int T, int S, int D) {
     BackwardPlan p{};
     Gradients &g = p.g;
     g.B = B; g.Bkv = B_kv; g.H = H; g.Hkv = H_kv; g.G = H / H_kv; g.T = T; g.S = S;
     g.share = B / B_kv;
     g.rows = g.share * g.G * T;
-    plan_cross_backward(&g);
+    plan_cross_backward(dtype, D, &g);
     const size_t q = sizeof(float) * (size_t)B * H * T * D, k = sizeof(float) * (size_t)B_kv * H_kv * S * D;
     p.dq = align256(sizeof(float) * 64 * (size_t)B * H * ((T + 31) / 32));
     p.dk = p.dq + (g.dq_pieces > 1 ? align256(q * g.dq_pieces) : 0);
@@ -86,7 +86,12 @@ extern "C" {
 
 size_t fibattn_cross_workspace_bytes(int B, int B_kv, int H, int H_kv, int T, int S, int d_head) {
     if (check_sizes(B, B_kv, H, H_kv, T, S, d_head, FIBATTN_BF16) != FIBATTN_OK) return 0;
-    return parts_bytes(forward_parts(B, B_kv, H, H_kv, T, S), (long long)B * H * T, d_head);
+    size_t most = 0;  // of both types
+    for (int t = 0; t < 2; ++t) {
+        const size_t x = parts_bytes(forward_parts(t, d_head, B, B_kv, H, H_kv, T, S), (long long)B * H * T, d_head);
+        most = x > most ? x : most;
+    }
+    return most;
 }
 
 fibattn_status_t fibattn_cross_forward(const void *q, const void *k, const void *v, void *o, float *lse,
@@ -105,7 +110,7 @@ fibattn_status_t fibattn_cross_forward(const void *q, const void *k, const void 
     a.lo = at.next(H, T);
     if (!at.ok) return FIBATTN_ERR_INVALID_ARG;
     if (!at.near) return FIBATTN_ERR_UNSUPPORTED;
-    const int parts = forward_parts(B, B_kv, H, H_kv, T, S);
+    const int parts = forward_parts((int)dtype, d_head, B, B_kv, H, H_kv, T, S);
     const size_t need = parts_bytes(parts, (long long)B * H * T, d_head);
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return FIBATTN_ERR_WORKSPACE;
     a.q = q; a.o = o; a.lse = lse;
@@ -121,7 +126,9 @@ fibattn_status_t fibattn_cross_forward(const void *q, const void *k, const void 
 
 size_t fibattn_cross_backward_workspace_bytes(int B, int B_kv, int H, int H_kv, int T, int S, int d_head) {
     if (check_sizes(B, B_kv, H, H_kv, T, S, d_head, FIBATTN_BF16) != FIBATTN_OK) return 0;
-    return plan_backward(B, B_kv, H, H_kv, T, S, d_head).total;
+    const size_t x = plan_backward(0, B, B_kv, H, H_kv, T, S, d_head).total;
+    const size_t y = plan_backward(1, B, B_kv, H, H_kv, T, S, d_head).total;
+    return x > y ? x : y;  // of both types
 }
 
 fibattn_status_t fibattn_cross_backward(const void *q, const void *k, const void *v, const void *o, const float *lse,
@@ -132,7 +139,7 @@ fibattn_status_t fibattn_cross_backward(const void *q, const void *k, const void
     fibattn_status_t st = check_sizes(B, B_kv, H, H_kv, T, S, d_head, dtype);
     if (st != FIBATTN_OK) return st;
     if (!all_aligned({q, k, v, o, (const void *)lse, dO, dq, dk, dv}) || !lens_ok(lens)) return FIBATTN_ERR_INVALID_ARG;
-    const BackwardPlan p = plan_backward(B, B_kv, H, H_kv, T, S, d_head);
+    const BackwardPlan p = plan_backward((int)dtype, B, B_kv, H, H_kv, T, S, d_head);
     if (!workspace || !aligned16(workspace) || workspace_bytes < p.total) return FIBATTN_ERR_WORKSPACE;
     Gradients g = p.g;
     Place at = {layouts, dtype, d_head, true, true};
@@ -164,8 +171,13 @@ size_t fibattn_prefix_workspace_bytes(int B, int H, int H_kv, int T, int P, int 
     if (check_sizes(B, 1, H, H_kv, T, P, d_head, FIBATTN_BF16) != FIBATTN_OK ||
         check_sizes(B, B, H, H_kv, T, S, d_head, FIBATTN_BF16) != FIBATTN_OK)
         return 0;
-    return parts_bytes(forward_parts(B, 1, H, H_kv, T, P) + forward_parts(B, B, H, H_kv, T, S), (long long)B * H * T,
-                       d_head);
+    size_t most = 0;  // of both types
+    for (int t = 0; t < 2; ++t) {
+        const int parts = forward_parts(t, d_head, B, 1, H, H_kv, T, P) + forward_parts(t, d_head, B, B, H, H_kv, T, S);
+        const size_t x = parts_bytes(parts, (long long)B * H * T, d_head);
+        most = x > most ? x : most;
+    }
+    return most;
 }
 
 fibattn_status_t fibattn_prefix_forward(const void *q, const void *k_prefix, const void *v_prefix, const void *k,
@@ -189,7 +201,8 @@ fibattn_status_t fibattn_prefix_forward(const void *q, const void *k_prefix, con
     a.lo = at.next(H, T);
     if (!at.ok) return FIBATTN_ERR_INVALID_ARG;
     if (!at.near) return FIBATTN_ERR_UNSUPPORTED;
-    const int parts = forward_parts(B, 1, H, H_kv, T, P) + forward_parts(B, B, H, H_kv, T, S);
+    const int parts = forward_parts((int)dtype, d_head, B, 1, H, H_kv, T, P) +
+                      forward_parts((int)dtype, d_head, B, B, H, H_kv, T, S);
     const size_t need = parts_bytes(parts, (long long)B * H * T, d_head);
     if (!workspace || !aligned16(workspace) || workspace_bytes < need) return FIBATTN_ERR_WORKSPACE;
     a.q = q; a.o = o; a.lse = lse;

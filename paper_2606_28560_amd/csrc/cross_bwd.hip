@@ -415,11 +415,11 @@ template <typename S, int D> struct KvItem {
 };
 
 // 128 rows of the states a workgroup, 32 to a wave with their k and v in registers; tiles of
-// 32 queries of one head (q, dO and their statistics) are staged for all four, two at a time.
+// 32 queries of one head (q, dO and their statistics) are staged for all four.
 template <typename S, int D>
 __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross_dkdv_kernel(Gradients a, int items) {
-    constexpr int QT = kStage<S> / 32, SB = 64 * Tile<S, D>::kRow + 256;
-    __shared__ __attribute__((aligned(16))) char lds[2 * QT * SB];
+    constexpr int SB = 64 * Tile<S, D>::kRow + 256;
+    __shared__ __attribute__((aligned(16))) char lds[2 * SB];
     const int blk = blockIdx.y * gridDim.x + blockIdx.x;
     if (blk >= items) return;
     const int item = xcd_item(blk, items);
@@ -431,35 +431,26 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) w.dk[dt] = w.dv[dt] = zero16();
     if (128 * tile < x.len) {
-        auto at = x.tile_at(a, x.n0);
-        auto fetch = [&](int i, int half) {
-#pragma unroll
-            for (int e = 0; e < QT; ++e)
-                if (i + e < x.n1) {
-                    char *dst = lds + (half * QT + e) * SB;
-                    x.template fetch_g<4>(a, at, dst, wv);
-                    x.template fetch_q<4>(a, at, dst, wv);
-                    x.step(a, at, 1);
-                }
+        auto at = x.tile_at(a, x.n0);  // of the tile that is fetched
+        auto fetch = [&](int half) {
+            x.template fetch_g<4>(a, at, lds + half * SB, wv);
+            x.template fetch_q<4>(a, at, lds + half * SB, wv);
+            x.step(a, at, 1);
         };
-        if (x.n0 < x.n1) fetch(x.n0, 0);
+        if (x.n0 < x.n1) fetch(0);
         x.load(a, w);
         wait_loads<0>();  // k and v too: no wait for them stays in the loop
         int half = 0;
-        for (int i = x.n0; i < x.n1; i += QT, half ^= 1) {
+        for (int i = x.n0; i < x.n1; ++i, half ^= 1) {
             wait_loads<0>();
             __syncthreads();  // this stage has arrived, the one before has been read
-            if (i + QT < x.n1) fetch(i + QT, half ^ 1);
+            if (i + 1 < x.n1) fetch(half ^ 1);
             if (idle) continue;
-#pragma unroll
-            for (int e = 0; e < QT; ++e) {
-                if (i + e >= x.n1) break;
-                const char *qt = lds + (half * QT + e) * SB;
-                f32x16_t s, u;
-                kv_products<S, D>(qt, a.scale, s, u, w);
-                kv_add_v<S, D>(qt, s, w);
-                kv_add_k<S, D>(qt, u, w);
-            }
+            const char *qt = lds + half * SB;
+            f32x16_t s, u;
+            kv_products<S, D>(qt, a.scale, s, u, w);
+            kv_add_v<S, D>(qt, s, w);
+            kv_add_k<S, D>(qt, u, w);
         }
     }
     x.template store<D>(a, 0, 0, w.dk, a.tau);
@@ -586,23 +577,45 @@ template <typename S> hipError_t backward_d(int D, const Gradients &a, hipStream
     }
 }
 
-// Workgroups of 128 rows or, where those are fewer than the CUs, narrow ones of 32; and in
-// how many pieces they take the other side's `steps` rows.
-constexpr int kFew = 256, kLeast = 256;
-void divide(long long prob, int rows, int steps, int *narrow, int *tiles, int *pieces) {
-    *narrow = prob * ((rows + 127) / 128) < kFew;
-    *tiles = (rows + (*narrow ? 31 : 127)) / (*narrow ? 32 : 128);
-    const long long wgs = prob * *tiles, want = (256 + wgs - 1) / wgs, most = (steps + kLeast - 1) / kLeast;
-    const long long n = want < most ? want : most;
-    *pieces = (int)(n < 1 ? 1 : n > 64 ? 64 : n);
+// Microseconds a wave needs for a tile of 32 x 32: dq, or dk and dv, while it has its SIMD
+// alone (of train_T1024's, d 128's and the float32 shapes' kernels).
+double tile_us(int dtype, int D, bool dkv) {
+    if (dtype == 1) return dkv ? 0.63 + 0.0112 * D : 0.75 + 0.003 * D;
+    return (dkv ? 0.07 : 0.053) * D;
+}
+
+// How a gradient over `rows` rows to a problem is computed: narrow workgroups (32 rows, the
+// other side's rows divided among the waves) or wide ones (128 rows), and in how many pieces
+// of the other side's `steps` rows: the least of an estimate of the time.
+void divide(int dtype, int D, long long prob, int rows, int steps, bool dkv, int *narrow, int *tiles, int *pieces) {
+    const double us = tile_us(dtype, D, dkv);
+    const int n = (steps + 31) / 32;
+    double best = 1e30;
+    for (int wide = 0; wide < 2; ++wide) {
+        const int t = (rows + (wide ? 127 : 31)) / (wide ? 128 : 32);
+        // float32 d 128 and the narrow kernel of bfloat16 d 128 leave no room for a second workgroup
+        const double second = D == 128 && (dtype == 0 || !wide) ? 1.0 : 0.75;
+        for (int p = 1; p <= 64 && p <= n; p += p < 4 ? 1 : p < 8 ? 2 : p < 16 ? 4 : 8) {
+            const int each = wide ? (n + p - 1) / p : (n + 4 * p - 1) / (4 * p);
+            const long long c = (prob * t * p + 255) / 256;  // workgroups to a CU
+            double x = (each * us + 3.0) * (c == 1 ? 1.0 : c * second);
+            if (p > 1) x += 3.0 + p * (dkv ? 2.0 : 1.0) * prob * rows * D * 8e-6 / 3.0;
+            if (x < best) {
+                best = x;
+                *narrow = !wide;
+                *tiles = t;
+                *pieces = p;
+            }
+        }
+    }
 }
 
 }  // namespace
 
-void plan_cross_backward(Gradients *a) {
+void plan_cross_backward(int dtype, int D, Gradients *a) {
     const long long prob = (long long)a->Bkv * a->Hkv;
-    divide(prob, a->rows, a->S, &a->dq_narrow, &a->row_tiles, &a->dq_pieces);
-    divide(prob, a->S, a->rows, &a->dkv_narrow, &a->key_tiles, &a->dkv_pieces);
+    divide(dtype, D, prob, a->rows, a->S, false, &a->dq_narrow, &a->row_tiles, &a->dq_pieces);
+    divide(dtype, D, prob, a->S, a->rows, true, &a->dkv_narrow, &a->key_tiles, &a->dkv_pieces);
 }
 
 hipError_t launch_cross_backward(int dtype, int D, const Gradients &a, hipStream_t s) {

@@ -498,18 +498,32 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
     if (d == 0) a.z[r] = sum == 0.f ? -INFINITY : m + __log2f(sum) * kLn2;
 }
 
-// Rows to a workgroup, row tiles and pieces of states for `prob` problems.  Few rows (at most
-// 32 to a problem) go to workgroups whose waves take different rows of the states.
-constexpr int kByKeys = 512;
-void plan(States *s, int prob) {
-    s->rw = s->rows <= kByKeys ? 0 : 4;
-    const int per = s->rw ? 32 * s->rw : 32;
-    s->tiles = (s->rows + per - 1) / per;
-    const long long wgs = (long long)prob * s->tiles;
-    // two workgroups to a CU; a piece keeps 256 rows or more
-    const long long want = (256 + wgs - 1) / wgs, most = (s->S + 255) / 256;
-    s->splits = (int)(want < 1 ? 1 : want < most ? want : most);
-    if (s->splits > 64) s->splits = 64;
+// By rows or by keys, row tiles and pieces of states for `prob` problems: the least of an
+// estimate of the time.  A wave takes 0.007 D microseconds for a tile of 32 x 32 in bfloat16,
+// 0.029 D in float32; two waves to a SIMD take 1.5 times as long as one.
+void plan(int dtype, int D, States *s, int prob) {
+    const double us = (dtype == 1 ? 0.007 : 0.029) * D, row = 2.0 * D * (dtype == 1 ? 2 : 4);
+    const int n = (s->S + 31) / 32;
+    double best = 1e30;
+    for (int rw = 0; rw <= 4; rw += 4) {
+        const int per = rw ? 128 : 32, t = (s->rows + per - 1) / per;
+        const double bytes = (double)prob * t * s->S * row;  // what the workgroups read, from L2 mostly
+        for (int p = 1; p <= 64 && p <= n; p += p < 4 ? 1 : p < 8 ? 2 : p < 16 ? 4 : 8) {
+            const long long c = ((long long)prob * t * p + 255) / 256;  // workgroups to a CU
+            const double each = rw ? 1.5 * us * ((n + 2 * p - 1) / (2 * p)) : us * ((n + 4 * p - 1) / (4 * p));
+            double x = (each + 3.0) * (c == 1 ? 1.0 : c * 0.75);
+            const double busy = c > 1 ? 1.0 : (double)prob * t * p / 256;
+            const double read = bytes / (t < 4 ? 5e6 : 1e7) / busy + 3.0;
+            if (read > x) x = read;
+            if (p > 1) x += 3.0 + p * (double)prob * s->rows * D * 8e-6 / 3.0;
+            if (x < best) {
+                best = x;
+                s->rw = rw;
+                s->tiles = t;
+                s->splits = p;
+            }
+        }
+    }
 }
 
 template <typename S, int D, int RW>
@@ -525,14 +539,15 @@ hipError_t launch_parts(const Queries &q, const States &s0, const States &s1, lo
 
 template <typename S, int D>
 hipError_t forward(const Queries &a, States s0, const States *s1, int prob0, int prob1, hipStream_t st) {
-    plan(&s0, prob0);
+    constexpr int dtype = sizeof(S) == 2;
+    plan(dtype, D, &s0, prob0);
     States own = s0;
     int parts = s0.splits;
     const long long n0 = (long long)prob0 * s0.tiles * s0.splits;
     long long n1 = 0;
     if (s1) {
         own = *s1;
-        plan(&own, prob1);
+        plan(dtype, D, &own, prob1);
         own.slot = parts;
         parts += own.splits;
         n1 = (long long)prob1 * own.tiles * own.splits;
@@ -569,11 +584,11 @@ template <typename S> hipError_t join_d(int D, const JoinArgs &a, hipStream_t st
 
 }  // namespace
 
-int cross_forward_parts(int rows, int S, int prob) {
+int cross_forward_parts(int dtype, int D, int rows, int S, int prob) {
     States s{};
     s.rows = rows;
     s.S = S;
-    plan(&s, prob);
+    plan(dtype, D, &s, prob);
     return s.splits;
 }
 

@@ -9,7 +9,7 @@ namespace fibattn {
 
 // Partial results the forward makes of each row over states of S rows, `rows` query rows to
 // each of `prob` problems.
-int cross_forward_parts(int rows, int S, int prob);
+int cross_forward_parts(int dtype, int D, int rows, int S, int prob);
 
 // Attention to s0 and, when s1 is not null, to s1 too, in one softmax; prob0, prob1: their
 // problems.  a.part_o and a.part_lse are read and written only where the pieces of both are
@@ -40,7 +40,7 @@ struct Gradients {
     int row_tiles, key_tiles, dq_pieces, dkv_pieces, dq_narrow, dkv_narrow;
     float scale, tau;  // tau log2 e, tau
 };
-void plan_cross_backward(Gradients *a);  // the tiles and pieces, from the sizes
+void plan_cross_backward(int dtype, int D, Gradients *a);  // the tiles and pieces, from the sizes
 hipError_t launch_cross_backward(int dtype, int D, const Gradients &a, hipStream_t s);
 
 }  // namespace fibattn
