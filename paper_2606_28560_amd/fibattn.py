@@ -9,6 +9,7 @@ raise.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from array import array
 
@@ -595,29 +596,29 @@ def fibattn_rope_qk_table(q, k, rope_base: float = 10000.0, *, theta=None, base=
 
 # ---- attention to states that are not the sequence's own ----------------------------
 
-def _rows(name, t, shape, like):
-    """t: [.., .., .., D] of `shape` with contiguous rows, of like's dtype and device."""
+def _rows(name, t, shape, dtype, dev):
+    """Whether t is packed; t: [.., .., .., D] of `shape` and dtype on GPU `dev`, rows contiguous."""
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if t.dtype != like.dtype:
-        raise ValueError(f"{name} has dtype {t.dtype}, expected {like.dtype}")
-    if t.device != like.device:
-        raise ValueError(f"{name} is on {t.device}, expected {like.device}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, expected cuda:{dev}")
+    if t.is_contiguous():
+        return True
     if t.stride(3) != 1:
         raise ValueError(f"{name} must have contiguous rows (last-dimension stride 1)")
+    return False
 
 
-def _vector(name, t, shape, dtype, like):
-    """t: a contiguous tensor of `shape` and dtype on like's device."""
-    if t.shape != shape or t.dtype != dtype or t.device != like.device or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on {like.device}")
+def _vector(name, t, shape, dtype, dev):
+    """t: a contiguous tensor of `shape` and dtype on GPU `dev`."""
+    if t.shape != shape or t.dtype != dtype or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor {tuple(shape)} on cuda:{dev}")
 
 
 def _places(*ts):
-    """Placements of the tensors (None where all are packed); a dimension of one element
-    has no stride of its own."""
-    if _packed(*ts):
-        return None
+    """Placements of the tensors; a dimension of one element has no stride of its own."""
     arr = (ctypes.c_int64 * (3 * len(ts)))()
     for a, t in enumerate(ts):
         for d in range(3):
@@ -625,41 +626,78 @@ def _places(*ts):
     return arr
 
 
-def _heads_of(q, k, B_kv):
-    if k.dim() != 4 or k.shape[3] != q.shape[3] or k.shape[1] < 1 or q.shape[1] % k.shape[1] or k.shape[0] not in B_kv:
-        raise ValueError(f"k: shape {tuple(k.shape)} does not group q {tuple(q.shape)}")
-    return q.shape[0], q.shape[1], k.shape[1], q.shape[2], k.shape[2], q.shape[3]
-
-
-def _at(t, stream):
+def _context(t, stream):
     """A context that makes t's device, and `stream` if given, current for the allocations
     and launches of a call (None: they are so already)."""
     import torch
 
-    if t.dim() != 4 or not t.is_cuda:
+    dev = t.get_device()
+    if dev < 0 or t.dim() != 4:
         raise ValueError("queries must be a GPU tensor [B,H,T,D]")
     if stream is not None:
         if stream.device != t.device:
             raise ValueError(f"stream is on {stream.device}, expected {t.device}")
         return torch.cuda.stream(stream)
-    if t.get_device() != torch.cuda.current_device():
-        return torch.cuda.device(t.device)
-    return None
+    return None if dev == torch._C._cuda_getDevice() else torch.cuda.device(dev)
 
 
-def _scratch(need, workspace, like):
-    """A workspace of `need` bytes: the caller's, or a new one."""
+def _raw_stream(dev):
+    import torch
+
+    return torch._C._cuda_getCurrentRawStream(dev)
+
+
+@functools.lru_cache(maxsize=256)
+def _workspace_bytes(fn, *sizes):
+    return int(getattr(lib(), fn)(*sizes))
+
+
+def _workspace(fn, sizes, workspace, like):
+    """(tensor that holds it, address, bytes) of a workspace: the caller's, or a new one."""
     if workspace is None:
+        need = _workspace_bytes(fn, *sizes)
+        if not need:
+            return None, None, 0
         import torch
 
-        return torch.empty(need, device=like.device, dtype=torch.uint8) if need else None
+        workspace = torch.empty(need, device=like.device, dtype=torch.uint8)
+        return workspace, workspace.data_ptr(), need
     if workspace.device != like.device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {like.device}")
-    return workspace
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
-def _bytes(workspace):
-    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+def _states_of(q, k, entries):
+    """B, B_kv, H, H_kv, T, S, D of queries [B,H,T,D] and states [B_kv,H_kv,S,D]."""
+    B, H, T, D = q.shape
+    shape = k.shape
+    if len(shape) != 4 or shape[3] != D or shape[1] < 1 or H % shape[1] or shape[0] not in entries:
+        raise ValueError(f"k: shape {tuple(shape)} does not group q {tuple(q.shape)}")
+    return B, shape[0], H, shape[1], T, shape[2], D
+
+
+def _outputs(q, o, lse, packed):
+    """o, lse (new where None) and whether o is packed too."""
+    import torch
+
+    if o is None:
+        o = torch.empty_like(q, memory_format=torch.contiguous_format)
+    else:
+        packed = _rows("o", o, q.shape, q.dtype, q.get_device()) and packed
+    if lse is None:
+        lse = torch.empty(q.shape[:3], device=q.device, dtype=torch.float32)
+    else:
+        _vector("lse", lse, q.shape[:3], torch.float32, q.get_device())
+    return o, lse, packed
+
+
+def _lens(lens, n, dev):
+    if lens is None:
+        return None
+    import torch
+
+    _vector("lens", lens, (n,), torch.int32, dev)
+    return lens.data_ptr()
 
 
 def fibattn_cross_workspace_bytes(B: int, B_kv: int, H: int, H_kv: int, T: int, S: int, d_head: int) -> int:
@@ -673,30 +711,20 @@ def fibattn_cross_forward(q, k, v, lens=None, *, o=None, lse=None, workspace=Non
     lens: int32 device tensor [B_kv] of valid rows (clamped to 0..S; rows behind them are
     not read), or None.  A sequence without a row gets o = 0, lse = -inf.  q, k, v, o may be
     views with contiguous 16-byte aligned rows; lse is packed float32 [B,H,T]."""
-    ctx = _at(q, stream)
+    ctx = _context(q, stream)
     if ctx is not None:
         with ctx:
             return fibattn_cross_forward(q, k, v, lens, o=o, lse=lse, workspace=workspace)
-    import torch
-
-    B, H, Hkv, T, S, D = _heads_of(q, k, (q.shape[0], 1))
-    dtype = _dtype_code(q)
-    if o is None:
-        o = torch.empty_like(q, memory_format=torch.contiguous_format)
-    for n_, t, sh in (("q", q, q.shape), ("k", k, k.shape), ("v", v, k.shape), ("o", o, q.shape)):
-        _rows(n_, t, sh, q)
-    if lse is None:
-        lse = torch.empty((B, H, T), device=q.device, dtype=torch.float32)
-    else:
-        _vector("lse", lse, (B, H, T), torch.float32, q)
-    if lens is not None:
-        _vector("lens", lens, (k.shape[0],), torch.int32, q)
-    L = lib()
-    sizes = (B, k.shape[0], H, Hkv, T, S, D)
-    workspace = _scratch(L.fibattn_cross_workspace_bytes(*sizes), workspace, q)
-    st = L.fibattn_cross_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
-                                 None if lens is None else lens.data_ptr(), *_bytes(workspace),
-                                 _places(q, k, v, o), *sizes, dtype, _stream(None))
+    sizes = _states_of(q, k, (q.shape[0], 1))
+    code, dtype, dev = _dtype_code(q), q.dtype, q.get_device()
+    packed = _rows("q", q, q.shape, dtype, dev) & _rows("k", k, k.shape, dtype, dev) & \
+        _rows("v", v, k.shape, dtype, dev)
+    o, lse, packed = _outputs(q, o, lse, packed)
+    n = _lens(lens, sizes[1], dev)
+    held, ws, ws_bytes = _workspace("fibattn_cross_workspace_bytes", sizes, workspace, q)
+    st = lib().fibattn_cross_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), n, ws,
+                                     ws_bytes, None if packed else _places(q, k, v, o), *sizes, code,
+                                     _raw_stream(dev))
     _check("fibattn_cross_forward", st)
     return o, lse
 
@@ -712,31 +740,30 @@ def fibattn_cross_backward(q, k, v, o, lse, dO, lens=None, *, dq=None, dk=None, 
     o and lse may be those of a softmax over more keys than these (fibattn_join): the
     gradients are then this part's share.  Every [..,D] tensor may be a view with contiguous
     16-byte aligned rows; new outputs are packed."""
-    ctx = _at(q, stream)
+    ctx = _context(q, stream)
     if ctx is not None:
         with ctx:
             return fibattn_cross_backward(q, k, v, o, lse, dO, lens, dq=dq, dk=dk, dv=dv, workspace=workspace)
     import torch
 
-    B, H, Hkv, T, S, D = _heads_of(q, k, (q.shape[0], 1))
-    dtype = _dtype_code(q)
-    packed = torch.contiguous_format
-    dq = torch.empty_like(q, memory_format=packed) if dq is None else dq
-    dk = torch.empty_like(k, memory_format=packed) if dk is None else dk
-    dv = torch.empty_like(k, memory_format=packed) if dv is None else dv
-    for n_, t, sh in (("q", q, q.shape), ("k", k, k.shape), ("v", v, k.shape), ("o", o, q.shape), ("dO", dO, q.shape),
-                      ("dq", dq, q.shape), ("dk", dk, k.shape), ("dv", dv, k.shape)):
-        _rows(n_, t, sh, q)
-    _vector("lse", lse, (B, H, T), torch.float32, q)
-    if lens is not None:
-        _vector("lens", lens, (k.shape[0],), torch.int32, q)
-    L = lib()
-    sizes = (B, k.shape[0], H, Hkv, T, S, D)
-    workspace = _scratch(L.fibattn_cross_backward_workspace_bytes(*sizes), workspace, q)
-    st = L.fibattn_cross_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
-                                  dO.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                  None if lens is None else lens.data_ptr(), *_bytes(workspace),
-                                  _places(q, k, v, o, dO, dq, dk, dv), *sizes, dtype, _stream(None))
+    sizes = _states_of(q, k, (q.shape[0], 1))
+    code, dtype, dev = _dtype_code(q), q.dtype, q.get_device()
+    fmt = torch.contiguous_format
+    packed = True
+    for name, t, shape in (("q", q, q.shape), ("k", k, k.shape), ("v", v, k.shape), ("o", o, q.shape),
+                           ("dO", dO, q.shape), ("dq", dq, q.shape), ("dk", dk, k.shape), ("dv", dv, k.shape)):
+        if t is not None:
+            packed &= _rows(name, t, shape, dtype, dev)
+    dq = torch.empty_like(q, memory_format=fmt) if dq is None else dq
+    dk = torch.empty_like(k, memory_format=fmt) if dk is None else dk
+    dv = torch.empty_like(k, memory_format=fmt) if dv is None else dv
+    _vector("lse", lse, q.shape[:3], torch.float32, dev)
+    n = _lens(lens, sizes[1], dev)
+    held, ws, ws_bytes = _workspace("fibattn_cross_backward_workspace_bytes", sizes, workspace, q)
+    st = lib().fibattn_cross_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+                                      dO.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), n, ws, ws_bytes,
+                                      None if packed else _places(q, k, v, o, dO, dq, dk, dv), *sizes, code,
+                                      _raw_stream(dev))
     _check("fibattn_cross_backward", st)
     return dq, dk, dv
 
@@ -753,35 +780,26 @@ def fibattn_prefix_forward(q, k_prefix, v_prefix, k, v, lens=None, *, o=None, ls
     lens: int32 device tensor [B] of valid own rows, the T new ones included (None: S);
     query t reads the own rows j <= lens[b] - T + t.  q, the four states and o may be views
     with contiguous 16-byte aligned rows."""
-    ctx = _at(q, stream)
+    ctx = _context(q, stream)
     if ctx is not None:
         with ctx:
             return fibattn_prefix_forward(q, k_prefix, v_prefix, k, v, lens, o=o, lse=lse, workspace=workspace)
-    import torch
-
-    B, H, Hkv, T, S, D = _heads_of(q, k, (q.shape[0],))
-    if k_prefix.dim() != 4 or k_prefix.shape[0] != 1 or k_prefix.shape[1] != Hkv or k_prefix.shape[3] != D:
-        raise ValueError(f"k_prefix has shape {tuple(k_prefix.shape)}, expected (1, {Hkv}, P, {D})")
-    P = k_prefix.shape[2]
-    dtype = _dtype_code(q)
-    if o is None:
-        o = torch.empty_like(q, memory_format=torch.contiguous_format)
-    for n_, t, sh in (("q", q, q.shape), ("k_prefix", k_prefix, k_prefix.shape),
-                      ("v_prefix", v_prefix, k_prefix.shape), ("k", k, k.shape), ("v", v, k.shape), ("o", o, q.shape)):
-        _rows(n_, t, sh, q)
-    if lse is None:
-        lse = torch.empty((B, H, T), device=q.device, dtype=torch.float32)
-    else:
-        _vector("lse", lse, (B, H, T), torch.float32, q)
-    if lens is not None:
-        _vector("lens", lens, (B,), torch.int32, q)
-    L = lib()
-    sizes = (B, H, Hkv, T, P, S, D)
-    workspace = _scratch(L.fibattn_prefix_workspace_bytes(*sizes), workspace, q)
-    st = L.fibattn_prefix_forward(q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                  o.data_ptr(), lse.data_ptr(), None if lens is None else lens.data_ptr(),
-                                  *_bytes(workspace), _places(q, k_prefix, v_prefix, k, v, o), *sizes, dtype,
-                                  _stream(None))
+    B, _, H, Hkv, T, S, D = _states_of(q, k, (q.shape[0],))
+    shape = k_prefix.shape
+    if len(shape) != 4 or shape[0] != 1 or shape[1] != Hkv or shape[3] != D:
+        raise ValueError(f"k_prefix has shape {tuple(shape)}, expected (1, {Hkv}, P, {D})")
+    sizes = (B, H, Hkv, T, shape[2], S, D)
+    code, dtype, dev = _dtype_code(q), q.dtype, q.get_device()
+    packed = _rows("q", q, q.shape, dtype, dev) & _rows("k_prefix", k_prefix, shape, dtype, dev) & \
+        _rows("v_prefix", v_prefix, shape, dtype, dev) & _rows("k", k, k.shape, dtype, dev) & \
+        _rows("v", v, k.shape, dtype, dev)
+    o, lse, packed = _outputs(q, o, lse, packed)
+    n = _lens(lens, B, dev)
+    held, ws, ws_bytes = _workspace("fibattn_prefix_workspace_bytes", sizes, workspace, q)
+    st = lib().fibattn_prefix_forward(q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k.data_ptr(),
+                                      v.data_ptr(), o.data_ptr(), lse.data_ptr(), n, ws, ws_bytes,
+                                      None if packed else _places(q, k_prefix, v_prefix, k, v, o), *sizes, code,
+                                      _raw_stream(dev))
     _check("fibattn_prefix_forward", st)
     return o, lse
 
@@ -793,23 +811,21 @@ def fibattn_join(o_a, lse_a, o_b, lse_b, *, o=None, lse=None, stream=None):
 
     The backward of each part with the joined o and lse gives that part's gradients: dq is
     the sum of the parts' dq (dalpha alone is not defined by one part's rows)."""
-    ctx = _at(o_a, stream)
+    ctx = _context(o_a, stream)
     if ctx is not None:
         with ctx:
             return fibattn_join(o_a, lse_a, o_b, lse_b, o=o, lse=lse)
     import torch
 
-    B, H, T, D = o_a.shape
-    dtype = _dtype_code(o_a)
-    if o is None:
-        o = torch.empty_like(o_a, memory_format=torch.contiguous_format)
-    for n_, t in (("o_a", o_a), ("o_b", o_b), ("o", o)):
-        _rows(n_, t, o_a.shape, o_a)
-    lse = torch.empty((B, H, T), device=o_a.device, dtype=torch.float32) if lse is None else lse
-    for n_, t in (("lse_a", lse_a), ("lse_b", lse_b), ("lse", lse)):
-        _vector(n_, t, (B, H, T), torch.float32, o_a)
+    B, H, T, D = shape = o_a.shape
+    code, dtype, dev = _dtype_code(o_a), o_a.dtype, o_a.get_device()
+    packed = _rows("o_a", o_a, shape, dtype, dev) & _rows("o_b", o_b, shape, dtype, dev)
+    _vector("lse_a", lse_a, shape[:3], torch.float32, dev)
+    _vector("lse_b", lse_b, shape[:3], torch.float32, dev)
+    o, lse, packed = _outputs(o_a, o, lse, packed)
     st = lib().fibattn_join(o_a.data_ptr(), lse_a.data_ptr(), o_b.data_ptr(), lse_b.data_ptr(), o.data_ptr(),
-                            lse.data_ptr(), _places(o_a, o_b, o), B, H, T, D, dtype, _stream(None))
+                            lse.data_ptr(), None if packed else _places(o_a, o_b, o), B, H, T, D, code,
+                            _raw_stream(dev))
     _check("fibattn_join", st)
     return o, lse
 
