@@ -9,13 +9,12 @@ namespace fibattn {
 namespace {
 
 // A workgroup of 8 waves on 32 RW query rows: RW waves side by side, KW = 8 / RW waves to the
-// same rows, each on its own 32 NS of the staged rows of the states.  Two waves to the same
-// rows double the waves a CU holds (MFMA and exponentials of one wave run beside another's)
-// without a result in memory; more of them serve problems of few rows.
+// same rows, each on its own 32 of the staged rows of the states.  Two waves to the same rows
+// double the waves a CU holds (MFMA and exponentials of one wave run beside another's)
+// without a result in memory.
 template <typename S, int D, int RW> struct Shape {
     static constexpr int KW = 8 / RW;
-    static constexpr int NS = KW == 2 && D * (int)sizeof(S) <= 128 ? 2 : 1;
-    static constexpr int NT = 32 * KW * NS;              // rows of a stage
+    static constexpr int NT = 32 * KW;                   // rows of a stage
     static constexpr int TB = NT * D * (int)sizeof(S);   // bytes of its k, and of its v
     static constexpr int merge = RW * (KW - 1) * 32 * (D + 2) * 4;
     static constexpr int lds = 4 * TB > merge ? 4 * TB : merge;
@@ -79,13 +78,11 @@ __device__ __forceinline__ void mask(f32x16_t &s, int base, const Rows<S, D> &w)
 
 // Logits to weights exp2(s - m).  The reference m moves only when a logit passes it by 8
 // powers of two: the sums keep their 24 bits and the accumulators are rarely rescaled.
-template <typename S, int D, int N>
-__device__ __forceinline__ void weights(f32x16_t *s, float scale, Rows<S, D> &w) {
-    float top = s[0][0];
+template <typename S, int D>
+__device__ __forceinline__ void weights(f32x16_t &s, float scale, Rows<S, D> &w) {
+    float top = s[0];
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[n][i]);
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = half_max(top) * scale;
     if (__ballot(top > w.m + 8.f)) {
         const float m = fmaxf(top, w.m);
@@ -98,12 +95,10 @@ __device__ __forceinline__ void weights(f32x16_t *s, float scale, Rows<S, D> &w)
     const float m = w.m == -INFINITY ? 0.f : w.m;
     float l = 0.f;
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            s[n][i] = ex2(fmaf(s[n][i], scale, -m));
-            l += s[n][i];
-        }
+    for (int i = 0; i < 16; ++i) {
+        s[i] = ex2(fmaf(s[i], scale, -m));
+        l += s[i];
+    }
     w.l += l;
 }
 
@@ -147,7 +142,7 @@ template <typename S, int D, int RW>
 __device__ __forceinline__ void rows_body(const Queries &a, const States &st, int item, char *lds, Redo &todo) {
     typedef Tile<S, D> X;
     typedef Shape<S, D, RW> Y;
-    constexpr int NT = Y::NT, NS = Y::NS, KW = Y::KW, TB = Y::TB;
+    constexpr int NT = Y::NT, KW = Y::KW, TB = Y::TB;
     const int lane = threadIdx.x & 63, h = lane >> 5, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rw = wv % RW, kw = wv / RW;
     const int tile = item % st.tiles, piece = item / st.tiles % st.splits, prob = item / st.tiles / st.splits;
@@ -175,19 +170,13 @@ __device__ __forceinline__ void rows_body(const Queries &a, const States &st, in
         wait_loads<0>();
         __syncthreads();  // this stage has arrived, the one before has been read
         if (i + 1 < n1) fetch(i + 1);
-        const int r = 32 * NS * kw, base = i * NT + r;
+        const int base = i * NT + 32 * kw;
         if (idle || base >= len) continue;
         const char *kt = lds + ((i - n0) & 1) * 2 * TB, *vt = kt + TB;
-        f32x16_t s[NS];
-#pragma unroll
-        for (int e = 0; e < NS; ++e) s[e] = logits<S, D>(kt, r + 32 * e, w);
-        if (base + 32 * NS > low) {
-#pragma unroll
-            for (int e = 0; e < NS; ++e) mask<S, D>(s[e], base + 32 * e, w);
-        }
-        weights<S, D, NS>(s, a.scale, w);
-#pragma unroll
-        for (int e = 0; e < NS; ++e) values<S, D>(vt, r + 32 * e, s[e], w);
+        f32x16_t s = logits<S, D>(kt, 32 * kw, w);
+        if (base + 32 > low) mask<S, D>(s, base, w);
+        weights<S, D>(s, a.scale, w);
+        values<S, D>(vt, 32 * kw, s, w);
     }
     float l = half_sum(w.l);
     if (KW > 1) {
@@ -275,7 +264,7 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
         wait_lds();  // K has been read
         if (more) X::template stage<32, 1>(kt, kp + 32 * (i + 4) * ks, ks, len - 32 * (i + 4), 0);
         if (32 * (i + 1) > low) mask<S, D>(s, 32 * i, w);
-        weights<S, D, 1>(&s, a.scale, w);
+        weights<S, D>(s, a.scale, w);
         if (more)
             wait_loads<OPS>();
         else
