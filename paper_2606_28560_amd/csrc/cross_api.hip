@@ -48,9 +48,23 @@ void place_parts(Queries *a, void *workspace, int parts, int D) {
     a->part_lse = parts < 2 ? nullptr : (float *)((char *)workspace + align256(sizeof(float) * parts * rows * D));
 }
 
-// Pieces of the forward over a batch's own states (B_kv = B) or shared ones (B_kv = 1).
-int forward_parts(int dtype, int D, int B, int B_kv, int H, int H_kv, int T, int S) {
-    return cross_forward_parts(dtype, D, B / B_kv * (H / H_kv) * T, S, B_kv * H_kv);
+// States of S rows for a batch of B: its own (B_kv = B) or shared ones (B_kv = 1).
+States states_of(int B, int B_kv, int H, int H_kv, int T, int S) {
+    States s{};
+    s.S = S;
+    s.share = B / B_kv;
+    s.rows = s.share * (H / H_kv) * T;
+    return s;
+}
+
+// Bytes of the partial results, of both types the larger.
+size_t forward_bytes(int D, const States &s0, const States *s1, int prob0, int prob1, long long rows) {
+    size_t most = 0;
+    for (int t = 0; t < 2; ++t) {
+        const size_t x = parts_bytes(cross_forward_parts(t, D, s0, s1, prob0, prob1), rows, D);
+        most = x > most ? x : most;
+    }
+    return most;
 }
 
 struct BackwardPlan {
@@ -86,12 +100,8 @@ extern "C" {
 
 size_t fibattn_cross_workspace_bytes(int B, int B_kv, int H, int H_kv, int T, int S, int d_head) {
     if (check_sizes(B, B_kv, H, H_kv, T, S, d_head, FIBATTN_BF16) != FIBATTN_OK) return 0;
-    size_t most = 0;  // of both types
-    for (int t = 0; t < 2; ++t) {
-        const size_t x = parts_bytes(forward_parts(t, d_head, B, B_kv, H, H_kv, T, S), (long long)B * H * T, d_head);
-        most = x > most ? x : most;
-    }
-    return most;
+    const States s = states_of(B, B_kv, H, H_kv, T, S);
+    return forward_bytes(d_head, s, nullptr, B_kv * H_kv, 0, (long long)B * H * T);
 }
 
 fibattn_status_t fibattn_cross_forward(const void *q, const void *k, const void *v, void *o, float *lse,
@@ -103,23 +113,21 @@ fibattn_status_t fibattn_cross_forward(const void *q, const void *k, const void 
     if (!all_aligned({q, k, v, o, (const void *)lse}) || !lens_ok(lens)) return FIBATTN_ERR_INVALID_ARG;
     Place at = {layouts, dtype, d_head, true, true};
     Queries a{};
-    States s{};
+    States s = states_of(B, B_kv, H, H_kv, T, S);
     a.lq = at.next(H, T);
     s.lk = at.next(H_kv, S);
     s.lv = at.next(H_kv, S);
     a.lo = at.next(H, T);
     if (!at.ok) return FIBATTN_ERR_INVALID_ARG;
     if (!at.near) return FIBATTN_ERR_UNSUPPORTED;
-    const int parts = forward_parts((int)dtype, d_head, B, B_kv, H, H_kv, T, S);
+    const int parts = cross_forward_parts((int)dtype, d_head, s, nullptr, B_kv * H_kv, 0);
     const size_t need = parts_bytes(parts, (long long)B * H * T, d_head);
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return FIBATTN_ERR_WORKSPACE;
     a.q = q; a.o = o; a.lse = lse;
     a.B = B; a.H = H; a.Hkv = H_kv; a.G = H / H_kv; a.T = T;
     a.scale = scale_of(d_head);
     place_parts(&a, workspace, parts, d_head);
-    s.k = k; s.v = v; s.lens = lens; s.S = S;
-    s.share = B / B_kv;
-    s.rows = s.share * a.G * T;
+    s.k = k; s.v = v; s.lens = lens;
     const hipError_t e = launch_cross_forward((int)dtype, d_head, a, s, nullptr, B_kv * H_kv, 0, stream);
     return e == hipSuccess ? FIBATTN_OK : FIBATTN_ERR_HIP;
 }
@@ -171,13 +179,8 @@ size_t fibattn_prefix_workspace_bytes(int B, int H, int H_kv, int T, int P, int 
     if (check_sizes(B, 1, H, H_kv, T, P, d_head, FIBATTN_BF16) != FIBATTN_OK ||
         check_sizes(B, B, H, H_kv, T, S, d_head, FIBATTN_BF16) != FIBATTN_OK)
         return 0;
-    size_t most = 0;  // of both types
-    for (int t = 0; t < 2; ++t) {
-        const int parts = forward_parts(t, d_head, B, 1, H, H_kv, T, P) + forward_parts(t, d_head, B, B, H, H_kv, T, S);
-        const size_t x = parts_bytes(parts, (long long)B * H * T, d_head);
-        most = x > most ? x : most;
-    }
-    return most;
+    const States pre = states_of(B, 1, H, H_kv, T, P), own = states_of(B, B, H, H_kv, T, S);
+    return forward_bytes(d_head, pre, &own, H_kv, B * H_kv, (long long)B * H * T);
 }
 
 fibattn_status_t fibattn_prefix_forward(const void *q, const void *k_prefix, const void *v_prefix, const void *k,
@@ -192,7 +195,7 @@ fibattn_status_t fibattn_prefix_forward(const void *q, const void *k_prefix, con
         return FIBATTN_ERR_INVALID_ARG;
     Place at = {layouts, dtype, d_head, true, true};
     Queries a{};
-    States pre{}, own{};
+    States pre = states_of(B, 1, H, H_kv, T, P), own = states_of(B, B, H, H_kv, T, S);
     a.lq = at.next(H, T);
     pre.lk = at.next(H_kv, P);
     pre.lv = at.next(H_kv, P);
@@ -201,20 +204,15 @@ fibattn_status_t fibattn_prefix_forward(const void *q, const void *k_prefix, con
     a.lo = at.next(H, T);
     if (!at.ok) return FIBATTN_ERR_INVALID_ARG;
     if (!at.near) return FIBATTN_ERR_UNSUPPORTED;
-    const int parts = forward_parts((int)dtype, d_head, B, 1, H, H_kv, T, P) +
-                      forward_parts((int)dtype, d_head, B, B, H, H_kv, T, S);
+    const int parts = cross_forward_parts((int)dtype, d_head, pre, &own, H_kv, B * H_kv);
     const size_t need = parts_bytes(parts, (long long)B * H * T, d_head);
     if (!workspace || !aligned16(workspace) || workspace_bytes < need) return FIBATTN_ERR_WORKSPACE;
     a.q = q; a.o = o; a.lse = lse;
     a.B = B; a.H = H; a.Hkv = H_kv; a.G = H / H_kv; a.T = T;
     a.scale = scale_of(d_head);
     place_parts(&a, workspace, parts, d_head);
-    pre.k = k_prefix; pre.v = v_prefix; pre.S = P;
-    pre.share = B;
-    pre.rows = B * a.G * T;
-    own.k = k; own.v = v; own.lens = lens; own.S = S;
-    own.share = 1;
-    own.rows = a.G * T;
+    pre.k = k_prefix; pre.v = v_prefix;
+    own.k = k; own.v = v; own.lens = lens;
     own.causal = 1;
     const hipError_t e = launch_cross_forward((int)dtype, d_head, a, pre, &own, H_kv, B * H_kv, stream);
     return e == hipSuccess ? FIBATTN_OK : FIBATTN_ERR_HIP;

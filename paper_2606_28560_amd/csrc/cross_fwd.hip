@@ -438,13 +438,19 @@ __global__ __launch_bounds__(256) void join_parts_kernel(Queries a, int parts) {
         const float f = z == -INFINITY ? 0.f : ex2((z - m) * kLog2e);
         sum += f;
         const float *x = a.part_o + ((long long)base * rows + r) * D + d;
-#pragma unroll 4
-        for (int i = g; i < (n + groups - 1) / groups * groups; i += groups) {
-            const float w = __shfl(f, i, 64);
-            f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-            if (i < n) v = *reinterpret_cast<const f32x4_t *>(x + (long long)i * rows * D);
+        for (int first = 0; first < n; first += 4 * groups) {
+            f32x4_t v[4];  // four parts on their way at a time
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] += w == 0.f ? 0.f : v[e] * w;
+            for (int u = 0; u < 4; ++u) {
+                const int i = first + u * groups + g;
+                v[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+                if (i < n) v[u] = *reinterpret_cast<const f32x4_t *>(x + (long long)i * rows * D);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float w = __shfl(f, min(first + u * groups + g, 63), 64);
+                if (first + u * groups + g < n && w != 0.f) y += v[u] * w;
+            }
         }
     }
 #pragma unroll
@@ -489,21 +495,25 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
 
 // By rows or by keys, row tiles and pieces of states for `prob` problems: the least of an
 // estimate of the time.  A wave takes 0.007 D microseconds for a tile of 32 x 32 in bfloat16,
-// 0.029 D in float32; two waves to a SIMD take 1.5 times as long as one.
-void plan(int dtype, int D, States *s, int prob) {
+// 0.029 D in float32; two waves to a SIMD take 1.5 times as long as one.  beside: how states of
+// the same call are read, whose launch these share if they are read so too (-1: none).
+void plan(int dtype, int D, States *s, int prob, int beside = -1) {
     const double us = (dtype == 1 ? 0.007 : 0.029) * D, row = 2.0 * D * (dtype == 1 ? 2 : 4);
     const int n = (s->S + 31) / 32;
     double best = 1e30;
     for (int rw = 0; rw <= 4; rw += 4) {
         const int per = rw ? 128 : 32, t = (s->rows + per - 1) / per;
-        const double bytes = (double)prob * t * s->S * row;  // what the workgroups read, from L2 mostly
+        // the states' rows, read once from memory and by every row tile from L2
+        const double once = (double)prob * s->S * row / 5e6, all = once * t * (5e6 / 1.2e7);
         for (int p = 1; p <= 64 && p <= n; p += p < 4 ? 1 : p < 8 ? 2 : p < 16 ? 4 : 8) {
             const long long c = ((long long)prob * t * p + 255) / 256;  // workgroups to a CU
             const double each = rw ? 1.5 * us * ((n + 2 * p - 1) / (2 * p)) : us * ((n + 4 * p - 1) / (4 * p));
-            double x = (each + 3.0) * (c == 1 ? 1.0 : c * 0.75);
+            // float32 rows of 128 leave no room for a second workgroup
+            double x = (each + 3.0) * (c == 1 ? 1.0 : c * (dtype == 0 && D == 128 ? 1.0 : 0.75));
             const double busy = c > 1 ? 1.0 : (double)prob * t * p / 256;
-            const double read = bytes / (t < 4 ? 5e6 : 1e7) / busy + 3.0;
+            const double read = (once > all ? once : all) / busy + 3.0;
             if (read > x) x = read;
+            if (beside >= 0 && rw != beside) x += 4.0;
             if (p > 1) x += 3.0 + p * (double)prob * s->rows * D * 8e-6 / 3.0;
             if (x < best) {
                 best = x;
@@ -529,22 +539,20 @@ hipError_t launch_parts(const Queries &q, const States &s0, const States &s1, lo
 template <typename S, int D>
 hipError_t forward(const Queries &a, States s0, const States *s1, int prob0, int prob1, hipStream_t st) {
     constexpr int dtype = sizeof(S) == 2;
-    plan(dtype, D, &s0, prob0);
     States own = s0;
-    int parts = s0.splits;
-    const long long n0 = (long long)prob0 * s0.tiles * s0.splits;
-    long long n1 = 0;
     if (s1) {
         own = *s1;
         plan(dtype, D, &own, prob1);
-        own.slot = parts;
-        parts += own.splits;
-        n1 = (long long)prob1 * own.tiles * own.splits;
     }
+    plan(dtype, D, &s0, prob0, s1 ? own.rw : -1);
+    own.slot = s0.splits;
+    const int parts = s0.splits + (s1 ? own.splits : 0);
+    const long long n0 = (long long)prob0 * s0.tiles * s0.splits;
+    const long long n1 = s1 ? (long long)prob1 * own.tiles * own.splits : 0;
     Queries q = a;
     if (parts == 1) q.part_o = q.part_lse = nullptr;
     // states that are read the same way share a launch
-    const bool both = own.rw == s0.rw;
+    const bool both = !s1 || own.rw == s0.rw;
     hipError_t e = launch_parts<S, D>(q, s0, own, n0, both ? n0 + n1 : n0, st);
     if (e == hipSuccess && !both) e = launch_parts<S, D>(q, own, own, n1, n1, st);
     if (e != hipSuccess || parts == 1) return e;
@@ -573,12 +581,14 @@ template <typename S> hipError_t join_d(int D, const JoinArgs &a, hipStream_t st
 
 }  // namespace
 
-int cross_forward_parts(int dtype, int D, int rows, int S, int prob) {
-    States s{};
-    s.rows = rows;
-    s.S = S;
-    plan(dtype, D, &s, prob);
-    return s.splits;
+int cross_forward_parts(int dtype, int D, const States &s0, const States *s1, int prob0, int prob1) {
+    States a = s0, own{};
+    if (s1) {
+        own = *s1;
+        plan(dtype, D, &own, prob1);
+    }
+    plan(dtype, D, &a, prob0, s1 ? own.rw : -1);
+    return a.splits + (s1 ? own.splits : 0);
 }
 
 hipError_t launch_cross_forward(int dtype, int D, const Queries &a, const States &s0, const States *s1, int prob0,

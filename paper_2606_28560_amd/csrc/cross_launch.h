@@ -7,9 +7,8 @@
 
 namespace fibattn {
 
-// Partial results the forward makes of each row over states of S rows, `rows` query rows to
-// each of `prob` problems.
-int cross_forward_parts(int dtype, int D, int rows, int S, int prob);
+// Partial results the forward makes of each row (the rows and S of the states are read).
+int cross_forward_parts(int dtype, int D, const States &s0, const States *s1, int prob0, int prob1);
 
 // Attention to s0 and, when s1 is not null, to s1 too, in one softmax; prob0, prob1: their
 // problems.  a.part_o and a.part_lse are read and written only where the pieces of both are
