@@ -148,16 +148,28 @@ __device__ __forceinline__ u32x4_t buffer_of(const void *src, uint32_t bytes) {
 }
 
 // Rows of D values staged in LDS: row-major, the 16-byte chunks of a row exchanged by an XOR
-// with swz(row).  Reading one chunk of 8 consecutive rows (row_frag) then touches every bank
-// once, and so do the transposed reads, which take 64 bytes of each of 4 consecutive rows.
+// with swz(row).  LDS serves 64 banks of 4 bytes a cycle: 16 lanes' chunks of 16 consecutive
+// rows (row_frag) and 64 bytes of each of 4 consecutive bfloat16 rows (operand_t) fall on
+// different banks.  bfloat16 rows of 128 values, 256 bytes, do so by an XOR within four rows
+// and 16 bytes between fours, which takes fewer addresses than an XOR alone.  Float32 rows
+// share some banks: their products, not their reads, take the time.
 template <typename S, int D> struct Tile {
     static constexpr int kRow = D * (int)sizeof(S);  // bytes of a row
     static constexpr int kChunks = kRow / 16;
     static constexpr int kRowsPerLoad = 1024 / kRow;  // rows a wave moves per instruction
+    static constexpr int kBlock = 1024 + (sizeof(S) == 2 && kChunks == 16 ? 16 : 0);  // bytes they take
+
+    static constexpr int bytes(int rows) { return rows / kRowsPerLoad * kBlock; }
 
     __device__ __forceinline__ static int swz(int row) {
-        if (kChunks == 4) return (row >> 1) & 3;
+        if (kChunks == 4) return (row >> 2) & 3;
+        if (kChunks == 8) return ((row & 2) << 1) | ((row & 4) >> 1) | ((row >> 3) & 1);
+        if (sizeof(S) == 2) return (row & 3) << 2;
         return ((row & 1) << 2) | (row & 2) | ((row >> 2) & 1);
+    }
+    // Chunk ch of a staged row.
+    __device__ __forceinline__ static const char *at(const char *t, int row, int ch) {
+        return t + row / kRowsPerLoad * kBlock + row % kRowsPerLoad * kRow + 16 * (ch ^ swz(row));
     }
 
     // Rows [0, N) at `src`, `stride` bytes apart (64 of them below 2^31 bytes), to `dst` by the
@@ -171,7 +183,7 @@ template <typename S, int D> struct Tile {
         const int rr = lane / kChunks, pc = lane % kChunks;
         const int st = (int)stride;
         const u32x4_t buf = buffer_of(src, (uint32_t)((min(valid, N) - 1) * st + kRow));
-        const uint32_t to = uniform(lds_address(dst) + 1024 * w);
+        const uint32_t to = uniform(lds_address(dst) + kBlock * w);
         int off[each];
 #pragma unroll
         for (int a = 0; a < each; ++a) {
@@ -180,21 +192,21 @@ template <typename S, int D> struct Tile {
         }
         if constexpr (each % 4 == 0) {
 #pragma unroll
-            for (int a = 0; a < each; a += 4) load_lds16(to + 1024 * NW * a, 1024 * NW, buf, off + a);
+            for (int a = 0; a < each; a += 4) load_lds16(to + kBlock * NW * a, kBlock * NW, buf, off + a);
         } else {
 #pragma unroll
             for (int a = 0; a < each; ++a)
-                if (loads % NW == 0 || a * NW + w < loads) load_lds16(to + 1024 * NW * a, buf, off[a]);
+                if (loads % NW == 0 || a * NW + w < loads) load_lds16(to + kBlock * NW * a, buf, off[a]);
         }
     }
 
     // Row `row`, step ks: values 16 ks + 8h .. + 7.
     __device__ __forceinline__ static void row_frag(const char *t, int row, int ks, int h, bf16x8_t &f) {
-        f = *reinterpret_cast<const bf16x8_t *>(t + row * kRow + 16 * ((2 * ks + h) ^ swz(row)));
+        f = *reinterpret_cast<const bf16x8_t *>(at(t, row, 2 * ks + h));
     }
     __device__ __forceinline__ static void row_frag(const char *t, int row, int ks, int h, f32x8_t &f) {
-        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(t + row * kRow + 16 * ((4 * ks + 2 * h) ^ swz(row)));
-        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(t + row * kRow + 16 * ((4 * ks + 2 * h + 1) ^ swz(row)));
+        const f32x4_t x = *reinterpret_cast<const f32x4_t *>(at(t, row, 4 * ks + 2 * h));
+        const f32x4_t y = *reinterpret_cast<const f32x4_t *>(at(t, row, 4 * ks + 2 * h + 1));
         f = f32x8_t{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
     }
 
@@ -210,7 +222,7 @@ template <typename S, int D> struct Tile {
         for (int j = 0; j < 2; ++j) {
             const int r = r0 + 8 * j + 4 * h + (m >> 2);
             x[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (__attribute__((address_space(3))) i16x4_t *)(t + r * kRow + 16 * (ch ^ swz(r)) + 8 * (m & 1)));
+                (__attribute__((address_space(3))) i16x4_t *)(at(t, r, ch) + 8 * (m & 1)));
         }
         f = __builtin_bit_cast(bf16x8_t, x);
     }
@@ -219,7 +231,7 @@ template <typename S, int D> struct Tile {
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
             const int r = r0 + 8 * (s >> 2) + 4 * h + (s & 3);
-            f[s] = *reinterpret_cast<const float *>(t + r * kRow + 16 * ((d >> 2) ^ swz(r)) + 4 * (d & 3));
+            f[s] = *reinterpret_cast<const float *>(at(t, r, d >> 2) + 4 * (d & 3));
         }
     }
 };

@@ -82,8 +82,8 @@ __device__ __forceinline__ void kv_products(const char *qt, float scale, f32x16_
                                             const KvRows<S, D> &w) {
     typedef Tile<S, D> X;
     const int lane = threadIdx.x & 63, h = lane >> 5;
-    const char *gt = qt + 32 * X::kRow;
-    const float *st = (const float *)(gt + 32 * X::kRow);
+    const char *gt = qt + X::bytes(32);
+    const float *st = (const float *)(gt + X::bytes(32));
     s = u = zero16();
 #pragma unroll
     for (int ks = 0; ks < D / 16; ++ks) {
@@ -117,7 +117,7 @@ __device__ __forceinline__ void kv_add_v(const char *qt, const f32x16_t &p, KvRo
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) {
             Frag<S> f;
-            Tile<S, D>::operand_t(qt + 32 * Tile<S, D>::kRow, 16 * x, dt, f);
+            Tile<S, D>::operand_t(qt + Tile<S, D>::bytes(32), 16 * x, dt, f);
             w.dv[dt] = pw.add(f, w.dv[dt]);
         }
     }
@@ -210,7 +210,7 @@ template <typename S, int D> struct DqItem {
 template <typename S, int D>
 __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross_dq_kernel(Gradients a, int items) {
     typedef Tile<S, D> X;
-    constexpr int NT = kStage<S>, TB = NT * X::kRow;
+    constexpr int NT = kStage<S>, TB = X::bytes(NT);
     __shared__ __attribute__((aligned(16))) char lds[4 * TB];
     const int blk = blockIdx.y * gridDim.x + blockIdx.x;
     if (blk >= items) return;
@@ -287,7 +287,7 @@ template <typename S> constexpr int kPrivate = sizeof(S) == 2 ? 2 : 1;
 template <typename S, int D>
 __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dq_narrow_kernel(Gradients a, int items) {
     typedef Tile<S, D> X;
-    constexpr int NB = kPrivate<S>, TB = 32 * X::kRow, N = D / 32;
+    constexpr int NB = kPrivate<S>, TB = X::bytes(32), N = D / 32;
     __shared__ __attribute__((aligned(16))) char lds[8 * NB * TB > 16384 * N ? 8 * NB * TB : 16384 * N];
     const int blk = blockIdx.y * gridDim.x + blockIdx.x;
     if (blk >= items) return;
@@ -385,7 +385,7 @@ template <typename S, int D> struct KvItem {
     template <int NW> __device__ __forceinline__ void fetch_g(const Gradients &a, const At &at, char *dst, int w) const {
         typedef Tile<S, D> X;
         const S *g = (const S *)a.g + (b0 + at.bb) * a.lg.sb + (j * a.G + at.g) * a.lg.sh + 32 * at.tt * a.lg.st;
-        X::template stage<32, NW>(dst + 32 * X::kRow, (const char *)g, a.lg.st * (long long)sizeof(S), a.T - 32 * at.tt, w);
+        X::template stage<32, NW>(dst + X::bytes(32), (const char *)g, a.lg.st * (long long)sizeof(S), a.T - 32 * at.tt, w);
     }
     template <int NW> __device__ __forceinline__ void fetch_q(const Gradients &a, const At &at, char *dst, int w) const {
         typedef Tile<S, D> X;
@@ -393,7 +393,7 @@ template <typename S, int D> struct KvItem {
         const S *q = (const S *)a.q + b * a.lq.sb + hh * a.lq.sh + 32 * at.tt * a.lq.st;
         X::template stage<32, NW>(dst, (const char *)q, a.lq.st * (long long)sizeof(S), a.T - 32 * at.tt, w);
         if (w == NW - 1)
-            load_lds4(uniform(lds_address(dst + 64 * X::kRow)),
+            load_lds4(uniform(lds_address(dst + 2 * X::bytes(32))),
                       buffer_of(a.stats + (((long long)b * a.H + hh) * tiles + at.tt) * 64, 256),
                       4 * (int)(threadIdx.x & 63));
     }
@@ -418,7 +418,7 @@ template <typename S, int D> struct KvItem {
 // 32 queries of one head (q, dO and their statistics) are staged for all four.
 template <typename S, int D>
 __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross_dkdv_kernel(Gradients a, int items) {
-    constexpr int SB = 64 * Tile<S, D>::kRow + 256;
+    constexpr int SB = 2 * Tile<S, D>::bytes(32) + 256;
     __shared__ __attribute__((aligned(16))) char lds[2 * SB];
     const int blk = blockIdx.y * gridDim.x + blockIdx.x;
     if (blk >= items) return;
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
 template <typename S, int D>
 __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dkdv_narrow_kernel(Gradients a, int items) {
     typedef Tile<S, D> X;
-    constexpr int NB = kPrivate<S>, N = D / 32, SB = 64 * X::kRow + 256;
+    constexpr int NB = kPrivate<S>, N = D / 32, SB = 2 * X::bytes(32) + 256;
     __shared__ __attribute__((aligned(16))) char lds[4 * NB * SB > 16384 * N ? 4 * NB * SB : 16384 * N];
     const int blk = blockIdx.y * gridDim.x + blockIdx.x;
     if (blk >= items) return;

@@ -15,14 +15,14 @@ namespace {
 template <typename S, int D, int RW> struct Shape {
     static constexpr int KW = 8 / RW;
     static constexpr int NT = 32 * KW;                   // rows of a stage
-    static constexpr int TB = NT * D * (int)sizeof(S);   // bytes of its k, and of its v
+    static constexpr int TB = Tile<S, D>::bytes(NT);     // bytes of its k, and of its v
     static constexpr int merge = RW * (KW - 1) * 32 * (D + 2) * 4;
     static constexpr int lds = 4 * TB > merge ? 4 * TB : merge;
 };
 
 template <typename S, int D> constexpr int keys_lds() {
     // per wave: K and V of 32 rows; at the end the waves' results
-    constexpr int waves = 4 * 2 * 32 * D * (int)sizeof(S), merge = 4 * 32 * D * 4;
+    constexpr int waves = 4 * 2 * Tile<S, D>::bytes(32), merge = 4 * 32 * D * 4;
     return waves > merge ? waves : merge;
 }
 
@@ -237,7 +237,7 @@ __device__ __forceinline__ void rows_body(const Queries &a, const States &st, in
 template <typename S, int D>
 __device__ __forceinline__ void keys_body(const Queries &a, const States &st, int item, char *lds, Redo &todo) {
     typedef Tile<S, D> X;
-    constexpr int TB = 32 * X::kRow, OPS = 32 / X::kRowsPerLoad;
+    constexpr int TB = X::bytes(32), OPS = 32 / X::kRowsPerLoad;
     __shared__ float stat[2][4][32];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int tile = item % st.tiles, piece = item / st.tiles % st.splits, prob = item / st.tiles / st.splits;
