@@ -597,8 +597,9 @@ def fibattn_rope_qk_table(q, k, rope_base: float = 10000.0, *, theta=None, base=
 # ---- attention to states that are not the sequence's own ----------------------------
 
 def _rows(name, t, shape, dtype, dev):
-    """Whether t is packed; t: [.., .., .., D] of `shape` and dtype on GPU `dev`, rows contiguous."""
-    if t.shape != shape:
+    """Whether t is packed; t: [.., .., .., D] of `shape` (None: checked already) and dtype on
+    GPU `dev`, rows contiguous."""
+    if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
     if t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, expected {dtype}")
@@ -667,17 +668,20 @@ def _workspace(fn, sizes, workspace, like):
     return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
-def _states_of(q, k, entries):
-    """B, B_kv, H, H_kv, T, S, D of queries [B,H,T,D] and states [B_kv,H_kv,S,D]."""
+def _states_of(q, k, shared):
+    """B, B_kv, H, H_kv, T, S, D of queries [B,H,T,D] and states [B_kv,H_kv,S,D]; B_kv is B
+    or, with `shared`, 1."""
     B, H, T, D = q.shape
-    shape = k.shape
-    if len(shape) != 4 or shape[3] != D or shape[1] < 1 or H % shape[1] or shape[0] not in entries:
-        raise ValueError(f"k: shape {tuple(shape)} does not group q {tuple(q.shape)}")
-    return B, shape[0], H, shape[1], T, shape[2], D
+    if k.dim() != 4:
+        raise ValueError(f"k: shape {tuple(k.shape)} does not group q {tuple(q.shape)}")
+    Bk, Hkv, S, Dk = k.shape
+    if Dk != D or Hkv < 1 or H % Hkv or not (Bk == B or shared and Bk == 1):
+        raise ValueError(f"k: shape {tuple(k.shape)} does not group q {tuple(q.shape)}")
+    return B, Bk, H, Hkv, T, S, D
 
 
-def _outputs(q, o, lse, packed):
-    """o, lse (new where None) and whether o is packed too."""
+def _outputs(q, shape, o, lse, packed):
+    """o, lse [B,H,T] of `shape` (new where None) and whether o is packed too."""
     import torch
 
     if o is None:
@@ -685,9 +689,9 @@ def _outputs(q, o, lse, packed):
     else:
         packed = _rows("o", o, q.shape, q.dtype, q.get_device()) and packed
     if lse is None:
-        lse = torch.empty(q.shape[:3], device=q.device, dtype=torch.float32)
+        lse = torch.empty(shape, device=q.device, dtype=torch.float32)
     else:
-        _vector("lse", lse, q.shape[:3], torch.float32, q.get_device())
+        _vector("lse", lse, shape, torch.float32, q.get_device())
     return o, lse, packed
 
 
@@ -715,11 +719,10 @@ def fibattn_cross_forward(q, k, v, lens=None, *, o=None, lse=None, workspace=Non
     if ctx is not None:
         with ctx:
             return fibattn_cross_forward(q, k, v, lens, o=o, lse=lse, workspace=workspace)
-    sizes = _states_of(q, k, (q.shape[0], 1))
+    sizes = _states_of(q, k, True)
     code, dtype, dev = _dtype_code(q), q.dtype, q.get_device()
-    packed = _rows("q", q, q.shape, dtype, dev) & _rows("k", k, k.shape, dtype, dev) & \
-        _rows("v", v, k.shape, dtype, dev)
-    o, lse, packed = _outputs(q, o, lse, packed)
+    packed = _rows("q", q, None, dtype, dev) & _rows("k", k, None, dtype, dev) & _rows("v", v, k.shape, dtype, dev)
+    o, lse, packed = _outputs(q, (sizes[0], sizes[2], sizes[4]), o, lse, packed)
     n = _lens(lens, sizes[1], dev)
     held, ws, ws_bytes = _workspace("fibattn_cross_workspace_bytes", sizes, workspace, q)
     st = lib().fibattn_cross_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), n, ws,
@@ -746,7 +749,7 @@ def fibattn_cross_backward(q, k, v, o, lse, dO, lens=None, *, dq=None, dk=None, 
             return fibattn_cross_backward(q, k, v, o, lse, dO, lens, dq=dq, dk=dk, dv=dv, workspace=workspace)
     import torch
 
-    sizes = _states_of(q, k, (q.shape[0], 1))
+    sizes = _states_of(q, k, True)
     code, dtype, dev = _dtype_code(q), q.dtype, q.get_device()
     fmt = torch.contiguous_format
     packed = True
@@ -784,16 +787,16 @@ def fibattn_prefix_forward(q, k_prefix, v_prefix, k, v, lens=None, *, o=None, ls
     if ctx is not None:
         with ctx:
             return fibattn_prefix_forward(q, k_prefix, v_prefix, k, v, lens, o=o, lse=lse, workspace=workspace)
-    B, _, H, Hkv, T, S, D = _states_of(q, k, (q.shape[0],))
+    B, _, H, Hkv, T, S, D = _states_of(q, k, False)
     shape = k_prefix.shape
     if len(shape) != 4 or shape[0] != 1 or shape[1] != Hkv or shape[3] != D:
         raise ValueError(f"k_prefix has shape {tuple(shape)}, expected (1, {Hkv}, P, {D})")
     sizes = (B, H, Hkv, T, shape[2], S, D)
     code, dtype, dev = _dtype_code(q), q.dtype, q.get_device()
-    packed = _rows("q", q, q.shape, dtype, dev) & _rows("k_prefix", k_prefix, shape, dtype, dev) & \
-        _rows("v_prefix", v_prefix, shape, dtype, dev) & _rows("k", k, k.shape, dtype, dev) & \
+    packed = _rows("q", q, None, dtype, dev) & _rows("k_prefix", k_prefix, None, dtype, dev) & \
+        _rows("v_prefix", v_prefix, shape, dtype, dev) & _rows("k", k, None, dtype, dev) & \
         _rows("v", v, k.shape, dtype, dev)
-    o, lse, packed = _outputs(q, o, lse, packed)
+    o, lse, packed = _outputs(q, (B, H, T), o, lse, packed)
     n = _lens(lens, B, dev)
     held, ws, ws_bytes = _workspace("fibattn_prefix_workspace_bytes", sizes, workspace, q)
     st = lib().fibattn_prefix_forward(q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k.data_ptr(),
@@ -819,10 +822,10 @@ def fibattn_join(o_a, lse_a, o_b, lse_b, *, o=None, lse=None, stream=None):
 
     B, H, T, D = shape = o_a.shape
     code, dtype, dev = _dtype_code(o_a), o_a.dtype, o_a.get_device()
-    packed = _rows("o_a", o_a, shape, dtype, dev) & _rows("o_b", o_b, shape, dtype, dev)
-    _vector("lse_a", lse_a, shape[:3], torch.float32, dev)
-    _vector("lse_b", lse_b, shape[:3], torch.float32, dev)
-    o, lse, packed = _outputs(o_a, o, lse, packed)
+    packed = _rows("o_a", o_a, None, dtype, dev) & _rows("o_b", o_b, shape, dtype, dev)
+    _vector("lse_a", lse_a, (B, H, T), torch.float32, dev)
+    _vector("lse_b", lse_b, (B, H, T), torch.float32, dev)
+    o, lse, packed = _outputs(o_a, (B, H, T), o, lse, packed)
     st = lib().fibattn_join(o_a.data_ptr(), lse_a.data_ptr(), o_b.data_ptr(), lse_b.data_ptr(), o.data_ptr(),
                             lse.data_ptr(), None if packed else _places(o_a, o_b, o), B, H, T, D, code,
                             _raw_stream(dev))
