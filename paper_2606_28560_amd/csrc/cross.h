@@ -3,9 +3,18 @@
 //
 // Every product runs on 32 x 32 matrix-core tiles.  A tile's operands hold, per lane, 8
 // values of one row: lane l serves row l % 32 and the inner indices 8h .. 8h + 7 of a step
-// of 16, h = l / 32 (Frag).  bfloat16 takes one v_mfma_f32_32x32x16_bf16 a step, float32
-// eight v_mfma_f32_32x32x2_f32 whose slot s pairs inner indices s and 8 + s.  The result
-// holds column l % 32 and rows 8 (i / 4) + 4h + i % 4, i < 16.
+// of 16, h = l / 32 (Frag), one v_mfma_f32_32x32x16_bf16 a step.  The result holds column
+// l % 32 and rows 8 (i / 4) + 4h + i % 4, i < 16.
+//
+// A float32 value goes as the sum of three bfloat16 ones, a = a0 + a1 + a2, each the rounded
+// rest of those before: |a1| <= 2^-8 |a|, |a2| <= 2^-16 |a|, and no rest stays (24 bits in
+// three times 8).  Of a product's nine partial products the six down to 2^-16 are taken, each
+// exact, summed in float32; the two largest of the others are at most 2^-24 of it.  Six
+// bfloat16 steps take 192 cycles of a matrix core where v_mfma_f32_32x32x2_f32 takes 512
+// (with the parts' making, forward and dq 1.2 to 1.35 times as fast, dk and dv 1.1 to 1.2 at
+// d 64 and 32).  The parts of d 128's rows of k and v are too many registers beside dk and dv:
+// those kernels take the float32 instructions (whole_t; 32 against 40 microseconds at 4 x 8
+// heads of 200 x 200).
 //
 // The kernels form the transposed logits, so that a lane holds one query's (dk, dv: one
 // key's) weights: of 16 consecutive inner rows its half h has rows 4h .. 4h + 3 and
@@ -28,12 +37,29 @@ typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
 
 template <typename S> struct FragOf;
 template <> struct FragOf<uint16_t> { typedef bf16x8_t type; };
-template <> struct FragOf<float> { typedef f32x8_t type; };
+struct bf16x8x3_t {
+    bf16x8_t p[3];
+};
+template <> struct FragOf<float> { typedef bf16x8x3_t type; };
+// float32 values that are multiplied whole: slot s of a step pairs inner indices s and 8 + s.
+struct whole_t {
+    float x;
+};
+template <> struct FragOf<whole_t> { typedef f32x8_t type; };
 template <typename S> using Frag = typename FragOf<S>::type;
 
 __device__ __forceinline__ f32x16_t mma(const bf16x8_t &a, const bf16x8_t &b, const f32x16_t &c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
+__device__ __forceinline__ f32x16_t mma(const bf16x8x3_t &a, const bf16x8x3_t &b, f32x16_t c) {
+    c = mma(a.p[2], b.p[0], c);  // the small ones first
+    c = mma(a.p[0], b.p[2], c);
+    c = mma(a.p[1], b.p[1], c);
+    c = mma(a.p[1], b.p[0], c);
+    c = mma(a.p[0], b.p[1], c);
+    return mma(a.p[0], b.p[0], c);
+}
+
 __device__ __forceinline__ f32x16_t mma(const f32x8_t &a, const f32x8_t &b, f32x16_t c) {
 #pragma unroll
     for (int s = 0; s < 8; ++s) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[s], b[s], c, 0, 0, 0);
@@ -49,33 +75,58 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_t));
 }
 
+// x in N bfloat16 parts.  (The rest of a rounding is a dot product with -1 and 0, and exact.)
+template <int N> __device__ __forceinline__ void split(const float *x, bf16x8_t *parts) {
+    uint32_t first = 0x0000bf80u, second = 0xbf800000u;  // (-1, 0), (0, -1): in registers, since
+    asm("" : "+s"(first), "+s"(second));  // as constants of the instruction they are read otherwise
+    uint32_t p[N][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float u = x[2 * i], v = x[2 * i + 1];
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            p[n][i] = pack2(u, v);
+            if (n == N - 1) break;
+            const bf16x2_t r = __builtin_bit_cast(bf16x2_t, p[n][i]);
+            u = __builtin_amdgcn_fdot2_f32_bf16(r, __builtin_bit_cast(bf16x2_t, first), u, false);
+            v = __builtin_amdgcn_fdot2_f32_bf16(r, __builtin_bit_cast(bf16x2_t, second), v, false);
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) parts[n] = __builtin_bit_cast(bf16x8_t, make_uint4(p[n][0], p[n][1], p[n][2], p[n][3]));
+}
+__device__ __forceinline__ void split(const f32x8_t &x, bf16x8x3_t &f) {
+    const float z[8] = {x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
+    split<3>(z, f.p);
+}
+
 // Values 8a .. 8a + 7 of a result as the operand of a step over its rows 16a .. 16a + 15.
 // A weight rounded to bfloat16 once is off by up to 2^-8, as much again as the rounding of a
-// stored output: bfloat16 weights go as two operands, the rounded weight and the rounded
-// rest (a dot product with -1 and 0 takes the difference, which is exact), good to 2^-16.
+// stored output: beside bfloat16 values weights go in two parts, good to 2^-16.
 template <typename S> struct Weights;
 template <> struct Weights<uint16_t> {
-    bf16x8_t hi, lo;
+    bf16x8_t p[2];
     __device__ __forceinline__ Weights(const f32x16_t &x, int a) {
-        uint32_t h[4], l[4];
-        uint32_t first = 0x0000bf80u, second = 0xbf800000u;  // (-1, 0), (0, -1): in registers, since
-        asm("" : "+s"(first), "+s"(second));  // as constants of the instruction they are read otherwise
+        float z[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float u = x[8 * a + 2 * i], v = x[8 * a + 2 * i + 1];
-            h[i] = pack2(u, v);
-            const bf16x2_t p = __builtin_bit_cast(bf16x2_t, h[i]);
-            l[i] = pack2(__builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf16x2_t, first), u, false),
-                         __builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf16x2_t, second), v, false));
-        }
-        hi = __builtin_bit_cast(bf16x8_t, make_uint4(h[0], h[1], h[2], h[3]));
-        lo = __builtin_bit_cast(bf16x8_t, make_uint4(l[0], l[1], l[2], l[3]));
+        for (int i = 0; i < 8; ++i) z[i] = x[8 * a + i];
+        split<2>(z, p);
     }
     __device__ __forceinline__ f32x16_t add(const bf16x8_t &f, const f32x16_t &c) const {
-        return mma(f, hi, mma(f, lo, c));
+        return mma(f, p[0], mma(f, p[1], c));
     }
 };
 template <> struct Weights<float> {
+    bf16x8x3_t w;
+    __device__ __forceinline__ Weights(const f32x16_t &x, int a) {
+        float z[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) z[i] = x[8 * a + i];
+        split<3>(z, w.p);
+    }
+    __device__ __forceinline__ f32x16_t add(const bf16x8x3_t &f, const f32x16_t &c) const { return mma(f, w, c); }
+};
+template <> struct Weights<whole_t> {
     f32x8_t w;
     __device__ __forceinline__ Weights(const f32x16_t &x, int a) {
 #pragma unroll
@@ -209,6 +260,11 @@ template <typename S, int D> struct Tile {
         const f32x4_t y = *reinterpret_cast<const f32x4_t *>(at(t, row, 4 * ks + 2 * h + 1));
         f = f32x8_t{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
     }
+    __device__ __forceinline__ static void row_frag(const char *t, int row, int ks, int h, bf16x8x3_t &f) {
+        f32x8_t x;
+        row_frag(t, row, ks, h, x);
+        split(x, f);
+    }
 
     // Column 32 dt + l % 32 of the 16 rows from r0 (a multiple of 16), in the order of a
     // result's rows: 4h .. 4h + 3, 8 + 4h .. 8 + 4h + 3.  bfloat16: two LDS transpose reads;
@@ -234,6 +290,11 @@ template <typename S, int D> struct Tile {
             f[s] = *reinterpret_cast<const float *>(at(t, r, d >> 2) + 4 * (d & 3));
         }
     }
+    __device__ __forceinline__ static void operand_t(const char *t, int r0, int dt, bf16x8x3_t &f) {
+        f32x8_t x;
+        operand_t(t, r0, dt, x);
+        split(x, f);
+    }
 };
 
 // Step ks of a row in global memory (rows are 16-byte aligned).
@@ -243,16 +304,24 @@ __device__ __forceinline__ void load_frag(const uint16_t *row, int ks, int h, bf
 __device__ __forceinline__ void load_frag(const float *row, int ks, int h, f32x8_t &f) {
     f = *reinterpret_cast<const f32x8_t *>(row + 16 * ks + 8 * h);
 }
-__device__ __forceinline__ float dot_frag(const bf16x8_t &a, const bf16x8_t &b) {
-    float s = 0.f;
+__device__ __forceinline__ void load_frag(const float *row, int ks, int h, bf16x8x3_t &f) {
+    f32x8_t x;
+    load_frag(row, ks, h, x);
+    split(x, f);
+}
+// Its inner product with the same step of another row.
+__device__ __forceinline__ float dot_rows(const uint16_t *a, const uint16_t *b, int ks, int h) {
+    float x[8], y[8], s = 0.f;
+    Vec<uint16_t>::load(a + 16 * ks + 8 * h, x);
+    Vec<uint16_t>::load(b + 16 * ks + 8 * h, y);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = fmaf((float)a[j], (float)b[j], s);
+    for (int j = 0; j < 8; ++j) s = fmaf(x[j], y[j], s);
     return s;
 }
-__device__ __forceinline__ float dot_frag(const f32x8_t &a, const f32x8_t &b) {
+__device__ __forceinline__ float dot_rows(const float *a, const float *b, int ks, int h) {
     float s = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = fmaf(a[j], b[j], s);
+    for (int j = 0; j < 8; ++j) s = fmaf(a[16 * ks + 8 * h + j], b[16 * ks + 8 * h + j], s);
     return s;
 }
 

@@ -70,7 +70,11 @@ __device__ __forceinline__ void dq_add(const char *kt, int row0, int base, int l
     }
 }
 
-// 32 rows of the states of a wave, and their gradients.
+// What the products of dk and dv take their operands from.
+template <typename S, int D> struct KvValue { typedef S type; };
+template <> struct KvValue<float, 128> { typedef whole_t type; };
+
+// 32 rows of the states of a wave, and their gradients (S: a KvValue).
 template <typename S, int D> struct KvRows {
     Frag<S> k[D / 16], v[D / 16];
     f32x16_t dk[D / 32], dv[D / 32];
@@ -170,11 +174,9 @@ template <typename S, int D> struct DqItem {
         float delta = 0.f;
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
-            Frag<S> f;
             load_frag(q, ks, h, w.q[ks]);
             load_frag(g, ks, h, w.g[ks]);
-            load_frag(o, ks, h, f);
-            delta += dot_frag(w.g[ks], f);
+            delta += dot_rows(g, o, ks, h);
         }
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) w.acc[dt] = zero16();
@@ -352,7 +354,7 @@ template <typename S, int D> struct KvItem {
         n0 = (int)((long long)n * piece / a.dkv_pieces);
         n1 = (int)((long long)n * (piece + 1) / a.dkv_pieces);
     }
-    __device__ __forceinline__ void load(const Gradients &a, KvRows<S, D> &w) const {
+    __device__ __forceinline__ void load(const Gradients &a, KvRows<typename KvValue<S, D>::type, D> &w) const {
         const int h = (threadIdx.x >> 5) & 1, cc = min(c, len - 1);
         const S *k = (const S *)a.k + b0 * a.lk.sb + j * a.lk.sh + cc * a.lk.st;
         const S *v = (const S *)a.v + b0 * a.lv.sb + j * a.lv.sh + cc * a.lv.st;
@@ -427,7 +429,8 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
     const int tile = item % a.key_tiles, piece = item / a.key_tiles % a.dkv_pieces;
     const KvItem<S, D> x(a, item / a.key_tiles / a.dkv_pieces, 128 * tile + 32 * wv, piece);
     const bool idle = 128 * tile + 32 * wv >= x.len;
-    KvRows<S, D> w;
+    typedef typename KvValue<S, D>::type V;
+    KvRows<V, D> w;
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) w.dk[dt] = w.dv[dt] = zero16();
     if (128 * tile < x.len) {
@@ -448,9 +451,9 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
             if (idle) continue;
             const char *qt = lds + half * SB;
             f32x16_t s, u;
-            kv_products<S, D>(qt, a.scale, s, u, w);
-            kv_add_v<S, D>(qt, s, w);
-            kv_add_k<S, D>(qt, u, w);
+            kv_products<V, D>(qt, a.scale, s, u, w);
+            kv_add_v<V, D>(qt, s, w);
+            kv_add_k<V, D>(qt, u, w);
         }
     }
     x.template store<D>(a, 0, 0, w.dk, a.tau);
@@ -470,7 +473,8 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dkdv_narrow_kerne
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int tile = item % a.key_tiles, piece = item / a.key_tiles % a.dkv_pieces;
     const KvItem<S, D> x(a, item / a.key_tiles / a.dkv_pieces, 32 * tile, piece);
-    KvRows<S, D> w;
+    typedef typename KvValue<S, D>::type V;
+    KvRows<V, D> w;
 #pragma unroll
     for (int dt = 0; dt < N; ++dt) w.dk[dt] = w.dv[dt] = zero16();
     if (32 * tile < x.len) {
@@ -494,13 +498,13 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dkdv_narrow_kerne
                 x.template fetch_q<1>(a, at, next, 0);
             }
             f32x16_t s, u;
-            kv_products<S, D>(qt, a.scale, s, u, w);
-            kv_add_v<S, D>(qt, s, w);
+            kv_products<V, D>(qt, a.scale, s, u, w);
+            kv_add_v<V, D>(qt, s, w);
             if (NB == 1 && more) {
                 wait_lds();  // dO has been read
                 x.template fetch_g<1>(a, at, qt, 0);
             }
-            kv_add_k<S, D>(qt, u, w);
+            kv_add_k<V, D>(qt, u, w);
             if (NB == 1 && more) {
                 wait_lds();  // q has been read
                 x.template fetch_q<1>(a, at, qt, 0);
@@ -581,7 +585,7 @@ template <typename S> hipError_t backward_d(int D, const Gradients &a, hipStream
 // alone (of train_T1024's, d 128's and the float32 shapes' kernels).
 double tile_us(int dtype, int D, bool dkv) {
     if (dtype == 1) return dkv ? 0.63 + 0.0112 * D : 0.75 + 0.003 * D;
-    return (dkv ? 0.07 : 0.053) * D;
+    return (dkv ? (D == 128 ? 0.07 : 0.062) : 0.042) * D;
 }
 
 // How a gradient over `rows` rows to a problem is computed: narrow workgroups (32 rows, the

@@ -402,7 +402,7 @@ template <typename S, int D, int RW> constexpr int body_lds() {
 // Waves to a SIMD that the registers are held down for.
 template <typename S, int D, int RW> constexpr int simd_waves() {
     if (sizeof(S) == 4 && D == 128) return RW ? 2 : 1;
-    return D <= 64 && RW ? 4 : 2;
+    return D * (int)sizeof(S) <= 128 && RW ? 4 : 2;
 }
 
 // Items [0, n0) of s0, then those of s1.
@@ -495,10 +495,10 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
 
 // By rows or by keys, row tiles and pieces of states for `prob` problems: the least of an
 // estimate of the time.  A wave takes 0.007 D microseconds for a tile of 32 x 32 in bfloat16,
-// 0.029 D in float32; two waves to a SIMD take 1.5 times as long as one.  beside: how states of
+// 0.022 D in float32; two waves to a SIMD take 1.5 times as long as one.  beside: how states of
 // the same call are read, whose launch these share if they are read so too (-1: none).
 void plan(int dtype, int D, States *s, int prob, int beside = -1) {
-    const double us = (dtype == 1 ? 0.007 : 0.029) * D, row = 2.0 * D * (dtype == 1 ? 2 : 4);
+    const double us = (dtype == 1 ? 0.007 : 0.022) * D, row = 2.0 * D * (dtype == 1 ? 2 : 4);
     const int n = (s->S + 31) / 32;
     double best = 1e30;
     for (int rw = 0; rw <= 4; rw += 4) {
