@@ -302,7 +302,8 @@ __device__ __forceinline__ void load_frag(const uint16_t *row, int ks, int h, bf
     f = *reinterpret_cast<const bf16x8_t *>(row + 16 * ks + 8 * h);
 }
 __device__ __forceinline__ void load_frag(const float *row, int ks, int h, f32x8_t &f) {
-    f = *reinterpret_cast<const f32x8_t *>(row + 16 * ks + 8 * h);
+    const f32x4_t *p = reinterpret_cast<const f32x4_t *>(row + 16 * ks + 8 * h);
+    f = f32x8_t{p[0][0], p[0][1], p[0][2], p[0][3], p[1][0], p[1][1], p[1][2], p[1][3]};
 }
 __device__ __forceinline__ void load_frag(const float *row, int ks, int h, bf16x8x3_t &f) {
     f32x8_t x;

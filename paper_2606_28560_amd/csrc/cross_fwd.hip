@@ -117,12 +117,14 @@ __device__ __forceinline__ void values(const char *vt, int row0, const f32x16_t 
 }
 
 // o and lse of a row (or its partial results), from the sum l over both halves.
-__device__ __forceinline__ void put_lse(const Queries &a, long long slot, long long id, float m, float l) {
-    const float z = l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2;
+__device__ __forceinline__ void store_lse(const Queries &a, long long slot, long long id, float z) {
     if (a.part_lse)
         a.part_lse[slot * a.B * a.H * a.T + id] = z;
     else
         a.lse[id] = z;
+}
+__device__ __forceinline__ void put_lse(const Queries &a, long long slot, long long id, float m, float l) {
+    store_lse(a, slot, id, l == 0.f ? -INFINITY : (m + __log2f(l)) * kLn2);
 }
 
 template <typename S, int D>
@@ -130,12 +132,18 @@ __device__ __forceinline__ S *out_row(const Queries &a, const RowAt &at) {
     return (S *)a.o + at.b * a.lo.sb + at.h * a.lo.sh + at.t * a.lo.st;
 }
 
-// Query rows first, first + step, .. below `end` of a problem over rows [c0, c1) of the states
-// that are to be done again (end 0: none).
+// Rows of a tile that are to be done again (bit i: row r0 + i), over rows [c0, c1) of the states.
 struct Redo {
-    int b0, j, first, step, end, c0, c1, len;
+    uint32_t which;
+    int b0, j, r0, c0, c1, len;
     long long slot;
 };
+// Whether a row's sum is one that the tiles may have made not finite: of the weights l, some of
+// its values' sums are not.  (A bfloat16 row whose weights are NaN met a NaN among what it reads;
+// a float32 one may have met an infinity, of which the parts of a value make a NaN.)
+template <typename S> __device__ __forceinline__ bool again(float values, float l) {
+    return !(fabsf(values) < INFINITY) && (sizeof(S) == 4 || l == l);
+}
 
 // 32 RW query rows, 32 to a wave; the waves share the staged rows of the states.
 template <typename S, int D, int RW>
@@ -215,16 +223,14 @@ __device__ __forceinline__ void rows_body(const Queries &a, const States &st, in
     }
     const float f = l == 0.f ? 0.f : 1.f / l;
     const long long slot = st.slot + piece;
-    float nan = 0.f;  // NaN if a value is (or an infinity)
+    float odd = 0.f;  // NaN if a value is not finite
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) nan = fmaf(w.acc[dt][e], 0.f, nan);
-    if (__ballot(w.on && nan != 0.f)) {
-        todo = {b0, j, r0, 1, r0 + 32, n0 * NT, min(n1 * NT, len), len, slot};
-        return;
-    }
-    if (!w.on) return;
+        for (int e = 0; e < 16; ++e) odd = fmaf(w.acc[dt][e], 0.f, odd);
+    const unsigned long long bad = __ballot(w.on && again<S>(odd, l));
+    if (bad) todo = {(uint32_t)(bad | bad >> 32), b0, j, r0, n0 * NT, min(n1 * NT, len), len, slot};
+    if (!w.on || (todo.which >> (lane & 31) & 1)) return;
     if (h == 0) put_lse(a, slot, w.id, w.m, l);
     if (a.part_o)
         store_cols<D>(a.part_o + (slot * a.B * a.H * a.T + w.id) * D, w.acc, f, h);
@@ -239,6 +245,7 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
     typedef Tile<S, D> X;
     constexpr int TB = X::bytes(32), OPS = 32 / X::kRowsPerLoad;
     __shared__ float stat[2][4][32];
+    __shared__ uint32_t odd_rows;
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int tile = item % st.tiles, piece = item / st.tiles % st.splits, prob = item / st.tiles / st.splits;
     const int b0 = prob / a.Hkv, j = prob % a.Hkv;
@@ -282,42 +289,54 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
         stat[0][wv][lane] = w.m;
         stat[1][wv][lane] = l;
     }
+    if (threadIdx.x == 0) odd_rows = 0;
     __syncthreads();
-    const long long slot = st.slot + piece;
-    constexpr int V = 4, per = D / V;  // lanes to a row
-    float nan = 0.f;  // NaN if a value is (or an infinity)
-    for (int e = threadIdx.x; e < 32 * per; e += 256) {
-        const int r = e / per, d = e % per * V;
-        if (32 * tile + r >= st.rows) continue;
+    constexpr int V = 4, per = D / V, each = 32 * per / 256;  // lanes to a row, values of a lane
+    f32x4_t y[each];
+    float lse[each];
+#pragma unroll
+    for (int e = 0; e < each; ++e) {
+        const int r = (threadIdx.x + 256 * e) / per, d = (threadIdx.x + 256 * e) % per * V;
         float m = stat[0][0][r];
 #pragma unroll
         for (int x = 1; x < 4; ++x) m = fmaxf(m, stat[0][x][r]);
         float sum = 0.f;
-        f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+        y[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
             // a wave that met no rows has the maximum -inf: it counts nothing
             const float f = stat[0][x][r] == -INFINITY ? 0.f : ex2(stat[0][x][r] - m);
             sum += stat[1][x][r] * f;
-            y += *reinterpret_cast<const f32x4_t *>(part + (32 * x + r) * D + d) * f;
+            y[e] += *reinterpret_cast<const f32x4_t *>(part + (32 * x + r) * D + d) * f;
         }
-        const float f = sum == 0.f ? 0.f : 1.f / sum;
-        nan = fmaf(y[0] + y[1] + y[2] + y[3], 0.f, nan);
+        if (again<S>((y[e][0] + y[e][1]) * 0.f + (y[e][2] + y[e][3]) * 0.f, sum)) atomicOr(&odd_rows, 1u << r);
+        y[e] *= sum == 0.f ? 0.f : 1.f / sum;
+        lse[e] = sum == 0.f ? -INFINITY : (m + __log2f(sum)) * kLn2;
+    }
+    __syncthreads();
+    const long long slot = st.slot + piece;
+    const uint32_t odd = odd_rows;
+#pragma unroll
+    for (int e = 0; e < each; ++e) {
+        const int r = (threadIdx.x + 256 * e) / per, d = (threadIdx.x + 256 * e) % per * V;
+        if (32 * tile + r >= st.rows || (odd >> r & 1)) continue;
         const RowAt at = row_at(a, b0, j, 32 * tile + r);
         const long long id = ((long long)at.b * a.H + at.h) * a.T + at.t;
-        if (d == 0) put_lse(a, slot, id, m, sum);
+        if (d == 0) store_lse(a, slot, id, lse[e]);
         if (a.part_o) {
-            *reinterpret_cast<f32x4_t *>(a.part_o + (slot * a.B * a.H * a.T + id) * D + d) = y * f;
+            *reinterpret_cast<f32x4_t *>(a.part_o + (slot * a.B * a.H * a.T + id) * D + d) = y[e];
         } else {
             S *row = out_row<S, D>(a, at) + d;
             if constexpr (sizeof(S) == 4)
-                *reinterpret_cast<f32x4_t *>(row) = y * f;
+                *reinterpret_cast<f32x4_t *>(row) = y[e];
             else
-                *reinterpret_cast<uint2 *>(row) = make_uint2(pack2(y[0] * f, y[1] * f), pack2(y[2] * f, y[3] * f));
+                *reinterpret_cast<uint2 *>(row) = make_uint2(pack2(y[e][0], y[e][1]), pack2(y[e][2], y[e][3]));
         }
     }
-    if (__syncthreads_or(nan != 0.f))
-        todo = {b0, j, 32 * tile + wv, 4, 32 * tile + 32, 32 * n0, min(32 * n1, len), len, slot};
+    // of the rows this problem has, a wave to every fourth
+    const int rows = st.rows - 32 * tile;
+    const uint32_t which = odd & (0x11111111u << wv) & (rows < 32 ? (1u << rows) - 1 : ~0u);
+    if (which) todo = {which, b0, j, 32 * tile, 32 * n0, min(32 * n1, len), len, slot};
 }
 
 __device__ __forceinline__ float value_of(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
@@ -325,53 +344,68 @@ __device__ __forceinline__ float value_of(float x) { return x; }
 __device__ __forceinline__ void put_value(uint16_t *p, float x) { *p = (uint16_t)f32_to_bf16(x); }
 __device__ __forceinline__ void put_value(float *p, float x) { *p = x; }
 
-// The rows of `todo`, each by the whole wave, one row of the states at a time and only those
-// it reads.
+// The rows of `todo`, each by the whole wave: a lane to each of 64 rows of the states, and only
+// to those that the query reads, for the weights; a lane to each value for the sums.
 //
-// The tiles multiply what a query does not read by a weight of 0, and a weight's bfloat16 rest
-// may be 0 or negative: with an infinity or NaN among the values either makes a NaN of what
-// is not one.  Rows whose tiles end in NaN are done again here, where nothing unread enters.
+// The tiles multiply what a query does not read by a weight of 0, and the rest of a weight may
+// be 0 or negative: with an infinity or NaN among the values either makes a NaN of what is not
+// one.  Here nothing unread enters, and every weight is whole.
 template <typename S, int D>
 __device__ __forceinline__ void plain_rows(const Queries &a, const States &st, const Redo &todo) {
-    const int b0 = todo.b0, j = todo.j, len = todo.len;
-    const long long slot = todo.slot;
-    constexpr int N = (D + 63) / 64;
+    constexpr int N = (D + 63) / 64, V = 16 / (int)sizeof(S);
     const int lane = threadIdx.x & 63;
-    const S *k = (const S *)st.k + b0 * st.lk.sb + j * st.lk.sh, *v = (const S *)st.v + b0 * st.lv.sb + j * st.lv.sh;
-    for (int r = todo.first; r < min(todo.end, st.rows); r += todo.step) {
-        const RowAt at = row_at(a, b0, j, r);
+    const S *k = (const S *)st.k + todo.b0 * st.lk.sb + todo.j * st.lk.sh;
+    const S *v = (const S *)st.v + todo.b0 * st.lv.sb + todo.j * st.lv.sh;
+    for (uint32_t left = todo.which; left; left &= left - 1) {
+        const RowAt at = row_at(a, todo.b0, todo.j, todo.r0 + __builtin_ctz(left));
         const long long id = ((long long)at.b * a.H + at.h) * a.T + at.t;
         const S *q = (const S *)a.q + at.b * a.lq.sb + at.h * a.lq.sh + at.t * a.lq.st;
-        const int lim = min(st.causal ? len - a.T + 1 + at.t : len, todo.c1);
-        float x[N], y[N], m = -INFINITY, l = 0.f;
+        const int lim = min(st.causal ? todo.len - a.T + 1 + at.t : todo.len, todo.c1);
+        float y[N], m = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            x[n] = lane + 64 * n < D ? value_of(q[lane + 64 * n]) : 0.f;
-            y[n] = 0.f;
-        }
-        for (int c = todo.c0; c < lim; ++c) {
-            float s = 0.f;
+        for (int n = 0; n < N; ++n) y[n] = 0.f;
+        for (int c = todo.c0; c < lim; c += 64) {
+            float s = -INFINITY;
+            if (c + lane < lim) {
+                s = 0.f;
+                for (int d = 0; d < D; d += V) {
+                    float x[V], z[V];
+                    Vec<S>::load(q + d, x);
+                    Vec<S>::load(k + (c + lane) * st.lk.st + d, z);
 #pragma unroll
-            for (int n = 0; n < N; ++n)
-                if (lane + 64 * n < D) s = fmaf(x[n], value_of(k[c * st.lk.st + lane + 64 * n]), s);
+                    for (int e = 0; e < V; ++e) s = fmaf(x[e], z[e], s);
+                }
+                s *= a.scale;
+            }
+            // a NaN stays one: fmaxf drops it, its weight below does not
+            float top = s;
 #pragma unroll
-            for (int e = 32; e; e >>= 1) s += __shfl_xor(s, e, 64);
-            s *= a.scale;
-            const float top = fmaxf(m, s), f = top == -INFINITY ? 1.f : ex2(m - top);
-            const float p = ex2(s - (top == -INFINITY ? 0.f : top));
+            for (int e = 32; e; e >>= 1) top = fmaxf(top, __shfl_xor(top, e, 64));
+            top = fmaxf(top, m);
+            const float f = top == -INFINITY ? 1.f : ex2(m - top);
+            const float p = c + lane < lim ? ex2(s - (top == -INFINITY ? 0.f : top)) : 0.f;
+            float sum = p;
+#pragma unroll
+            for (int e = 32; e; e >>= 1) sum += __shfl_xor(sum, e, 64);
             m = top;
-            l = fmaf(l, f, p);
+            l = fmaf(l, f, sum);
 #pragma unroll
-            for (int n = 0; n < N; ++n)
-                if (lane + 64 * n < D) y[n] = fmaf(p, value_of(v[c * st.lv.st + lane + 64 * n]), y[n] * f);
+            for (int n = 0; n < N; ++n) y[n] *= f;
+            const int count = min(64, lim - c);
+            for (int e = 0; e < count; ++e) {
+                const float w = __shfl(p, e, 64);
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+                    if (lane + 64 * n < D) y[n] = fmaf(w, value_of(v[(c + e) * st.lv.st + lane + 64 * n]), y[n]);
+            }
         }
         const float f = l == 0.f ? 0.f : 1.f / l;
-        if (lane == 0) put_lse(a, slot, id, m, l);
+        if (lane == 0) put_lse(a, todo.slot, id, m, l);
 #pragma unroll
         for (int n = 0; n < N; ++n)
             if (lane + 64 * n < D) {
                 if (a.part_o)
-                    a.part_o[(slot * a.B * a.H * a.T + id) * D + lane + 64 * n] = y[n] * f;
+                    a.part_o[(todo.slot * a.B * a.H * a.T + id) * D + lane + 64 * n] = y[n] * f;
                 else
                     put_value(out_row<S, D>(a, at) + lane + 64 * n, y[n] * f);
             }
@@ -379,17 +413,15 @@ __device__ __forceinline__ void plain_rows(const Queries &a, const States &st, c
 }
 
 // By rows (RW > 0: 8 waves) or by keys (RW 0: 4 waves).
-template <typename S, int D, int RW> constexpr int waves_of() { return RW ? 8 : 4; }
-
 template <typename S, int D, int RW>
 __device__ __forceinline__ void body(const Queries &a, const States &st, int item, char *lds) {
     Redo todo;
-    todo.end = 0;
+    todo.which = 0;
     if constexpr (RW == 0)
         keys_body<S, D>(a, st, item, lds, todo);
     else
         rows_body<S, D, RW>(a, st, item, lds, todo);
-    if (todo.end) plain_rows<S, D>(a, st, todo);
+    if (todo.which) plain_rows<S, D>(a, st, todo);
 }
 
 template <typename S, int D, int RW> constexpr int body_lds() {

@@ -128,6 +128,39 @@ def test_not_finite_values():
     assert int(torch.isnan(o).sum()) == 64 and int(torch.isnan(lse).sum()) == 1
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("T", [1, 40, 700])
+def test_not_finite_values_of_every_path(dtype, T):
+    """An infinite value, and a NaN in one query, in a long call in pieces, and in one by rows."""
+    B, H, Hkv, S, D = 1, 2, 1, 1500, 64
+    q, k, v, _ = _inputs(dtype, B, B, H, Hkv, T, S, D, seed=45)
+    clean, lse0 = F.fibattn_cross_forward(q, k, v)
+    v[0, 0, 700, 5] = math.inf
+    q[0, 1, T - 1, 0] = math.nan
+    o, lse = F.fibattn_cross_forward(q, k, v)
+    bad = torch.zeros((B, H, T), dtype=torch.bool, device="cuda")
+    bad[0, 1, T - 1] = True
+    assert bool(torch.isnan(o[bad]).all()) and bool(torch.isnan(lse[bad]).all())
+    assert bool((o[~bad][:, 5] == math.inf).all())
+    ref = R.attention(q.nan_to_num(), k, torch.where(torch.isinf(v), torch.zeros_like(v), v))
+    rest = (o.double() - ref["o"]).abs() <= ref["e_o"]
+    rest[..., 5] = True
+    assert bool(rest[~bad].all())
+    assert bool(((lse.double() - ref["lse"]).abs() <= ref["e_lse"])[~bad].all())
+
+
+def test_infinite_keys():
+    """A float32 key of -inf that every query weighs with 0, beside finite ones."""
+    q, k, v, _ = _inputs(FP, 1, 1, 1, 1, 3, 70, 32, seed=47)
+    q[..., 0] = 1.0
+    k[0, 0, 9] = 0.0
+    k[0, 0, 9, 0] = -math.inf
+    o, lse = F.fibattn_cross_forward(q, k, v)
+    keep = torch.ones((1, 3, 70), dtype=torch.bool, device="cuda")
+    keep[:, :, 9] = False
+    R.check({"o": o, "lse": lse}, R.attention(q, k, v, keep=keep), "infinite key")
+
+
 def test_large_logits():
     """Weights that all but one row round to 0, and a maximum that keeps moving."""
     q, k, v, dO = _inputs(FP, 1, 1, 1, 1, 64, 512, 64, seed=50)
