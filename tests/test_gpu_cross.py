@@ -83,6 +83,36 @@ def test_forward_and_gradients(case):
 
 @pytest.mark.parametrize("dtype", [BF, FP])
 @pytest.mark.parametrize("D", [32, 64, 128])
+def test_many_rows(dtype, D):
+    """Enough rows on one side or both for the kernels by 128 rows, odd sizes, ragged lengths."""
+    for B, H, Hkv, T, S, lens in ((4, 8, 4, 1001, 1030, [1030, 0, 1, 777]), (8, 8, 8, 90, 1024, None),
+                                  (8, 8, 8, 1023, 90, None)):
+        q, k, v, dO = _inputs(dtype, B, B, H, Hkv, T, S, D, seed=15)
+        n = _lens(lens)
+        ref = R.attention(q, k, v, dO, None if n is None else R.lens_mask(n, T, S))
+        o, lse = F.fibattn_cross_forward(q, k, v, n)
+        R.check({"o": o, "lse": lse}, ref, "forward")
+        dq, dk, dv = F.fibattn_cross_backward(q, k, v, o, lse, dO, n)
+        R.check({"dq": dq, "dk": dk, "dv": dv}, ref, "backward")
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_few_rows_of_long_states(dtype, D):
+    """States divided into pieces in both directions, and one row of them beside many queries."""
+    for B, Bk, H, Hkv, T, S, lens in ((1, 1, 2, 1, 5, 3001, [2999]), (3, 1, 2, 2, 900, 1, None),
+                                      (2, 2, 1, 1, 40, 1600, [1600, 31])):
+        q, k, v, dO = _inputs(dtype, B, Bk, H, Hkv, T, S, D, seed=16)
+        n = _lens(lens)
+        ref = R.attention(q, k, v, dO, None if n is None else R.lens_mask(n, T, S))
+        o, lse = F.fibattn_cross_forward(q, k, v, n)
+        R.check({"o": o, "lse": lse}, ref, "forward")
+        dq, dk, dv = F.fibattn_cross_backward(q, k, v, o, lse, dO, n)
+        R.check({"dq": dq, "dk": dk, "dv": dv}, ref, "backward")
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("D", [32, 64, 128])
 def test_placements(dtype, D):
     """q, k, v, o, dO and the gradients inside larger buffers; what is around them stays."""
     B, H, Hkv, T, S = 2, 4, 2, 67, 150
