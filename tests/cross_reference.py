@@ -5,7 +5,8 @@ A value computed as sum_j w_j x_j with weights rounded to the storage type (rela
 u, at most half a step: 2^-8 in bfloat16, none in float32), summed in float32 and stored
 (relative error us: 2^-8 or 2^-24) is off by at most (u + g) sum |w_j x_j| + us |value|.
 g = n 2^-24 counts the float32 operations one after the other: n terms of the sums, and the
-error of a logit, whose products and exponent add (D + 8) 2^-24 tau sum |q_i k_i| to it.
+error of a logit, whose products and exponent add (D + 8) 2^-24 tau sum |q_i k_i| to it
+(float32 products of three bfloat16 parts, two of the nine left out at 2^-24 each, among them).
 The gradient's Delta = <dO, o> takes the stored o, so that o's own bound enters dS.
 """
 import math
