@@ -58,10 +58,10 @@ States states_of(int B, int B_kv, int H, int H_kv, int T, int S) {
 }
 
 // Bytes of the partial results, of both types the larger.
-size_t forward_bytes(int D, const States &s0, const States *s1, int prob0, int prob1, long long rows) {
+size_t forward_bytes(int D, States s0, States *s1, int prob0, int prob1, long long rows) {
     size_t most = 0;
     for (int t = 0; t < 2; ++t) {
-        const size_t x = parts_bytes(cross_forward_parts(t, D, s0, s1, prob0, prob1), rows, D);
+        const size_t x = parts_bytes(plan_cross_forward(t, D, &s0, s1, prob0, prob1), rows, D);
         most = x > most ? x : most;
     }
     return most;
@@ -120,7 +120,7 @@ fibattn_status_t fibattn_cross_forward(const void *q, const void *k, const void 
     a.lo = at.next(H, T);
     if (!at.ok) return FIBATTN_ERR_INVALID_ARG;
     if (!at.near) return FIBATTN_ERR_UNSUPPORTED;
-    const int parts = cross_forward_parts((int)dtype, d_head, s, nullptr, B_kv * H_kv, 0);
+    const int parts = plan_cross_forward((int)dtype, d_head, &s, nullptr, B_kv * H_kv, 0);
     const size_t need = parts_bytes(parts, (long long)B * H * T, d_head);
     if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return FIBATTN_ERR_WORKSPACE;
     a.q = q; a.o = o; a.lse = lse;
@@ -179,8 +179,8 @@ size_t fibattn_prefix_workspace_bytes(int B, int H, int H_kv, int T, int P, int 
     if (check_sizes(B, 1, H, H_kv, T, P, d_head, FIBATTN_BF16) != FIBATTN_OK ||
         check_sizes(B, B, H, H_kv, T, S, d_head, FIBATTN_BF16) != FIBATTN_OK)
         return 0;
-    const States pre = states_of(B, 1, H, H_kv, T, P), own = states_of(B, B, H, H_kv, T, S);
-    return forward_bytes(d_head, pre, &own, H_kv, B * H_kv, (long long)B * H * T);
+    States own = states_of(B, B, H, H_kv, T, S);
+    return forward_bytes(d_head, states_of(B, 1, H, H_kv, T, P), &own, H_kv, B * H_kv, (long long)B * H * T);
 }
 
 fibattn_status_t fibattn_prefix_forward(const void *q, const void *k_prefix, const void *v_prefix, const void *k,
@@ -204,7 +204,7 @@ fibattn_status_t fibattn_prefix_forward(const void *q, const void *k_prefix, con
     a.lo = at.next(H, T);
     if (!at.ok) return FIBATTN_ERR_INVALID_ARG;
     if (!at.near) return FIBATTN_ERR_UNSUPPORTED;
-    const int parts = cross_forward_parts((int)dtype, d_head, pre, &own, H_kv, B * H_kv);
+    const int parts = plan_cross_forward((int)dtype, d_head, &pre, &own, H_kv, B * H_kv);
     const size_t need = parts_bytes(parts, (long long)B * H * T, d_head);
     if (!workspace || !aligned16(workspace) || workspace_bytes < need) return FIBATTN_ERR_WORKSPACE;
     a.q = q; a.o = o; a.lse = lse;

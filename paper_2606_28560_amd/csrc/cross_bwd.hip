@@ -613,6 +613,7 @@ void divide(int dtype, int D, long long prob, int rows, int steps, bool dkv, int
         for (int p = 1; p <= 64 && p <= n; p += p < 4 ? 1 : p < 8 ? 2 : p < 16 ? 4 : 8) {
             const int each = wide ? (n + p - 1) / p : (n + 4 * p - 1) / (4 * p);
             const long long c = (prob * t * p + 255) / 256;  // workgroups to a CU
+            if (p > 1 && c > 8) break;  // there are enough without more pieces
             double x = (each * us + 3.0) * (c == 1 ? 1.0 : c * second);
             if (p > 1) x += 3.0 + p * (dkv ? 2.0 : 1.0) * prob * rows * D * 8e-6 / 3.0;
             if (x < best) {

@@ -541,6 +541,7 @@ void plan(int dtype, int D, States *s, int prob, int beside = -1) {
         const double once = (double)prob * s->S * row / 5e6, all = once * t * (5e6 / 1.2e7);
         for (int p = 1; p <= 64 && p <= n; p += p < 4 ? 1 : p < 8 ? 2 : p < 16 ? 4 : 8) {
             const long long c = ((long long)prob * t * p + 255) / 256;  // workgroups to a CU
+            if (p > 1 && c > 8) break;  // there are enough without more pieces
             const double each = rw ? 1.5 * us * ((n + 2 * p - 1) / (2 * p)) : us * ((n + 4 * p - 1) / (4 * p));
             // float32 rows of 128 leave no room for a second workgroup
             double x = (each + 3.0) * (c == 1 ? 1.0 : c * (dtype == 0 && D == 128 ? 1.0 : 0.75));
@@ -571,18 +572,11 @@ hipError_t launch_parts(const Queries &q, const States &s0, const States &s1, lo
 }
 
 template <typename S, int D>
-hipError_t forward(const Queries &a, States s0, const States *s1, int prob0, int prob1, hipStream_t st) {
-    constexpr int dtype = sizeof(S) == 2;
-    States own = s0;
-    if (s1) {
-        own = *s1;
-        plan(dtype, D, &own, prob1);
-    }
-    plan(dtype, D, &s0, prob0, s1 ? own.rw : -1);
-    own.slot = s0.splits;
-    const int parts = s0.splits + (s1 ? own.splits : 0);
+hipError_t forward(const Queries &a, const States &s0, const States *s1, int prob0, int prob1, hipStream_t st) {
+    const int parts = s0.splits + (s1 ? s1->splits : 0);
     const long long n0 = (long long)prob0 * s0.tiles * s0.splits;
-    const long long n1 = s1 ? (long long)prob1 * own.tiles * own.splits : 0;
+    const long long n1 = s1 ? (long long)prob1 * s1->tiles * s1->splits : 0;
+    const States &own = s1 ? *s1 : s0;
     Queries q = a;
     if (parts == 1) q.part_o = q.part_lse = nullptr;
     // states that are read the same way share a launch
@@ -615,14 +609,13 @@ template <typename S> hipError_t join_d(int D, const JoinArgs &a, hipStream_t st
 
 }  // namespace
 
-int cross_forward_parts(int dtype, int D, const States &s0, const States *s1, int prob0, int prob1) {
-    States a = s0, own{};
-    if (s1) {
-        own = *s1;
-        plan(dtype, D, &own, prob1);
-    }
-    plan(dtype, D, &a, prob0, s1 ? own.rw : -1);
-    return a.splits + (s1 ? own.splits : 0);
+int plan_cross_forward(int dtype, int D, States *s0, States *s1, int prob0, int prob1) {
+    if (s1) plan(dtype, D, s1, prob1);
+    plan(dtype, D, s0, prob0, s1 ? s1->rw : -1);
+    s0->slot = 0;
+    if (!s1) return s0->splits;
+    s1->slot = s0->splits;
+    return s0->splits + s1->splits;
 }
 
 hipError_t launch_cross_forward(int dtype, int D, const Queries &a, const States &s0, const States *s1, int prob0,

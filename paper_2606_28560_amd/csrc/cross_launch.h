@@ -7,11 +7,12 @@
 
 namespace fibattn {
 
-// Partial results the forward makes of each row (the rows and S of the states are read).
-int cross_forward_parts(int dtype, int D, const States &s0, const States *s1, int prob0, int prob1);
+// How the forward reads the states (rw, tiles, splits, slot, from their rows and S); the partial
+// results it makes of each row.  s1: null, or the second states.
+int plan_cross_forward(int dtype, int D, States *s0, States *s1, int prob0, int prob1);
 
-// Attention to s0 and, when s1 is not null, to s1 too, in one softmax; prob0, prob1: their
-// problems.  a.part_o and a.part_lse are read and written only where the pieces of both are
+// Attention to s0 and, when s1 is not null, to s1 too, in one softmax, as planned; prob0, prob1:
+// their problems.  a.part_o and a.part_lse are read and written only where the pieces of both are
 // more than one.
 hipError_t launch_cross_forward(int dtype, int D, const Queries &a, const States &s0, const States *s1, int prob0,
                                 int prob1, hipStream_t s);

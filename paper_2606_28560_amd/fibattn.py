@@ -627,12 +627,11 @@ def _places(*ts):
     return arr
 
 
-def _context(t, stream):
-    """A context that makes t's device, and `stream` if given, current for the allocations
+def _elsewhere(t, dev, stream):
+    """A context that makes t's GPU `dev`, and `stream` if given, current for the allocations
     and launches of a call (None: they are so already)."""
     import torch
 
-    dev = t.get_device()
     if dev < 0 or t.dim() != 4:
         raise ValueError("queries must be a GPU tensor [B,H,T,D]")
     if stream is not None:
@@ -661,7 +660,7 @@ def _workspace(fn, sizes, workspace, like):
             return None, None, 0
         import torch
 
-        workspace = torch.empty(need, device=like.device, dtype=torch.uint8)
+        workspace = like.new_empty(need, dtype=torch.uint8)
         return workspace, workspace.data_ptr(), need
     if workspace.device != like.device or not workspace.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on {like.device}")
@@ -680,18 +679,18 @@ def _states_of(q, k, shared):
     return B, Bk, H, Hkv, T, S, D
 
 
-def _outputs(q, shape, o, lse, packed):
-    """o, lse [B,H,T] of `shape` (new where None) and whether o is packed too."""
+def _outputs(q, shape, o, lse, dev, packed):
+    """o, lse [B,H,T] of `shape` (new where None) and whether q's placement `packed` is o's too."""
     import torch
 
     if o is None:
         o = torch.empty_like(q, memory_format=torch.contiguous_format)
     else:
-        packed = _rows("o", o, q.shape, q.dtype, q.get_device()) and packed
+        packed = _rows("o", o, q.shape, q.dtype, dev) and packed
     if lse is None:
-        lse = torch.empty(shape, device=q.device, dtype=torch.float32)
+        lse = q.new_empty(shape, dtype=torch.float32)
     else:
-        _vector("lse", lse, shape, torch.float32, q.get_device())
+        _vector("lse", lse, shape, torch.float32, dev)
     return o, lse, packed
 
 
@@ -715,14 +714,15 @@ def fibattn_cross_forward(q, k, v, lens=None, *, o=None, lse=None, workspace=Non
     lens: int32 device tensor [B_kv] of valid rows (clamped to 0..S; rows behind them are
     not read), or None.  A sequence without a row gets o = 0, lse = -inf.  q, k, v, o may be
     views with contiguous 16-byte aligned rows; lse is packed float32 [B,H,T]."""
-    ctx = _context(q, stream)
+    dev = q.get_device()
+    ctx = _elsewhere(q, dev, stream)
     if ctx is not None:
         with ctx:
             return fibattn_cross_forward(q, k, v, lens, o=o, lse=lse, workspace=workspace)
     sizes = _states_of(q, k, True)
-    code, dtype, dev = _dtype_code(q), q.dtype, q.get_device()
+    code, dtype = _dtype_code(q), q.dtype
     packed = _rows("q", q, None, dtype, dev) & _rows("k", k, None, dtype, dev) & _rows("v", v, k.shape, dtype, dev)
-    o, lse, packed = _outputs(q, (sizes[0], sizes[2], sizes[4]), o, lse, packed)
+    o, lse, packed = _outputs(q, (sizes[0], sizes[2], sizes[4]), o, lse, dev, packed)
     n = _lens(lens, sizes[1], dev)
     held, ws, ws_bytes = _workspace("fibattn_cross_workspace_bytes", sizes, workspace, q)
     st = lib().fibattn_cross_forward(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), n, ws,
@@ -743,14 +743,15 @@ def fibattn_cross_backward(q, k, v, o, lse, dO, lens=None, *, dq=None, dk=None, 
     o and lse may be those of a softmax over more keys than these (fibattn_join): the
     gradients are then this part's share.  Every [..,D] tensor may be a view with contiguous
     16-byte aligned rows; new outputs are packed."""
-    ctx = _context(q, stream)
+    dev = q.get_device()
+    ctx = _elsewhere(q, dev, stream)
     if ctx is not None:
         with ctx:
             return fibattn_cross_backward(q, k, v, o, lse, dO, lens, dq=dq, dk=dk, dv=dv, workspace=workspace)
     import torch
 
     sizes = _states_of(q, k, True)
-    code, dtype, dev = _dtype_code(q), q.dtype, q.get_device()
+    code, dtype = _dtype_code(q), q.dtype
     fmt = torch.contiguous_format
     packed = True
     for name, t, shape in (("q", q, q.shape), ("k", k, k.shape), ("v", v, k.shape), ("o", o, q.shape),
@@ -783,7 +784,8 @@ def fibattn_prefix_forward(q, k_prefix, v_prefix, k, v, lens=None, *, o=None, ls
     lens: int32 device tensor [B] of valid own rows, the T new ones included (None: S);
     query t reads the own rows j <= lens[b] - T + t.  q, the four states and o may be views
     with contiguous 16-byte aligned rows."""
-    ctx = _context(q, stream)
+    dev = q.get_device()
+    ctx = _elsewhere(q, dev, stream)
     if ctx is not None:
         with ctx:
             return fibattn_prefix_forward(q, k_prefix, v_prefix, k, v, lens, o=o, lse=lse, workspace=workspace)
@@ -792,11 +794,11 @@ def fibattn_prefix_forward(q, k_prefix, v_prefix, k, v, lens=None, *, o=None, ls
     if len(shape) != 4 or shape[0] != 1 or shape[1] != Hkv or shape[3] != D:
         raise ValueError(f"k_prefix has shape {tuple(shape)}, expected (1, {Hkv}, P, {D})")
     sizes = (B, H, Hkv, T, shape[2], S, D)
-    code, dtype, dev = _dtype_code(q), q.dtype, q.get_device()
+    code, dtype = _dtype_code(q), q.dtype
     packed = _rows("q", q, None, dtype, dev) & _rows("k_prefix", k_prefix, None, dtype, dev) & \
         _rows("v_prefix", v_prefix, shape, dtype, dev) & _rows("k", k, None, dtype, dev) & \
         _rows("v", v, k.shape, dtype, dev)
-    o, lse, packed = _outputs(q, (B, H, T), o, lse, packed)
+    o, lse, packed = _outputs(q, (B, H, T), o, lse, dev, packed)
     n = _lens(lens, B, dev)
     held, ws, ws_bytes = _workspace("fibattn_prefix_workspace_bytes", sizes, workspace, q)
     st = lib().fibattn_prefix_forward(q.data_ptr(), k_prefix.data_ptr(), v_prefix.data_ptr(), k.data_ptr(),
@@ -814,18 +816,19 @@ def fibattn_join(o_a, lse_a, o_b, lse_b, *, o=None, lse=None, stream=None):
 
     The backward of each part with the joined o and lse gives that part's gradients: dq is
     the sum of the parts' dq (dalpha alone is not defined by one part's rows)."""
-    ctx = _context(o_a, stream)
+    dev = o_a.get_device()
+    ctx = _elsewhere(o_a, dev, stream)
     if ctx is not None:
         with ctx:
             return fibattn_join(o_a, lse_a, o_b, lse_b, o=o, lse=lse)
     import torch
 
     B, H, T, D = shape = o_a.shape
-    code, dtype, dev = _dtype_code(o_a), o_a.dtype, o_a.get_device()
+    code, dtype = _dtype_code(o_a), o_a.dtype
     packed = _rows("o_a", o_a, None, dtype, dev) & _rows("o_b", o_b, shape, dtype, dev)
     _vector("lse_a", lse_a, (B, H, T), torch.float32, dev)
     _vector("lse_b", lse_b, (B, H, T), torch.float32, dev)
-    o, lse, packed = _outputs(o_a, (B, H, T), o, lse, packed)
+    o, lse, packed = _outputs(o_a, (B, H, T), o, lse, dev, packed)
     st = lib().fibattn_join(o_a.data_ptr(), lse_a.data_ptr(), o_b.data_ptr(), lse_b.data_ptr(), o.data_ptr(),
                             lse.data_ptr(), None if packed else _places(o_a, o_b, o), B, H, T, D, code,
                             _raw_stream(dev))
