@@ -34,7 +34,7 @@ struct Gradients {
     void *dq, *dk, *dv;
     Layout lq, lk, lv, lo, lg, ldq, ldk, ldv;
     const int *lens;
-    float *stats;  // per tile of 32 positions of a head: lse log2 e of each, then <dO, o>
+    float *stats;  // per tile of 32 positions of a head: lse log2 e of each, then -<dO, o>
     float *dq_part, *dk_part, *dv_part;  // [piece][rows][D] where a sum is made in pieces
     int B, Bkv, H, Hkv, G, T, S, share, rows;  // share: B where Bkv is 1, else 1; rows: share G T
     int row_tiles, key_tiles, dq_pieces, dkv_pieces, dq_narrow, dkv_narrow;
