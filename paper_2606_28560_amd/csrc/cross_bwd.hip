@@ -243,21 +243,23 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
 
     const int n = (len + NT - 1) / NT;
     const int n0 = (int)((long long)n * piece / a.dq_pieces), n1 = (int)((long long)n * (piece + 1) / a.dq_pieces);
-    auto fetch = [&](int i) {
+    auto fetch = [&](int i, int half) {
         const int row = i * NT;
-        char *dst = lds + ((i - n0) & 1) * 2 * TB;
+        char *dst = lds + half * 2 * TB;
         X::template stage<NT, 4>(dst, x.kp + row * x.ks, x.ks, len - row, wv);
         X::template stage<NT, 4>(dst + TB, x.vp + row * x.vs, x.vs, len - row, wv);
     };
-    if (n0 < n1) fetch(n0);
+    if (n0 < n1) fetch(n0, 0);
     x.load(a, piece == 0, w);
     wait_loads<0>();  // the queries too: no wait for them stays in the loop
-    for (int i = n0; i < n1; ++i) {
+    // one stage from half `half` of the LDS; two to a turn of the loop, so that their addresses
+    // are constants (-1 to -2 %)
+    auto step = [&](int i, int half) {
         wait_loads<0>();
         __syncthreads();  // this stage has arrived, the one before has been read
-        if (i + 1 < n1) fetch(i + 1);
-        if (idle) continue;
-        const char *kt = lds + ((i - n0) & 1) * 2 * TB;
+        if (i + 1 < n1) fetch(i + 1, half ^ 1);
+        if (idle) return;
+        const char *kt = lds + half * 2 * TB;
 #pragma unroll
         for (int e = 0; e < NT / 32; ++e)
             if (i * NT + 32 * e < len) {
@@ -265,6 +267,10 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
                 dq_products<S, D>(kt, kt + TB, 32 * e, s, u, w);
                 dq_add<S, D>(kt, 32 * e, i * NT + 32 * e, len, a.scale, s, u, w);
             }
+    };
+    for (int i = n0; i < n1; i += 2) {
+        step(i, 0);
+        if (i + 1 < n1) step(i + 1, 1);
     }
     x.template store<D>(a, 0, w.acc);
 }
@@ -460,17 +466,21 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
         if (x.n0 < x.n1) fetch(0);
         x.load(a, w);
         wait_loads<0>();  // k and v too: no wait for them stays in the loop
-        int half = 0;
-        for (int i = x.n0; i < x.n1; ++i, half ^= 1) {
+        // one stage, as in dq
+        auto step = [&](int i, int half) {
             wait_loads<0>();
             __syncthreads();  // this stage has arrived, the one before has been read
             if (i + 1 < x.n1) fetch(half ^ 1);
-            if (idle) continue;
+            if (idle) return;
             const char *qt = lds + half * SB;
             f32x16_t s, u;
             kv_products<V, D>(qt, a.scale, s, u, w);
             kv_add_v<V, D>(qt, s, w);
             kv_add_k<V, D>(qt, u, w);
+        };
+        for (int i = x.n0; i < x.n1; i += 2) {
+            step(i, 0);
+            if (i + 1 < x.n1) step(i + 1, 1);
         }
     }
     x.template store<D>(a, 0, 0, w.dk, a.tau);

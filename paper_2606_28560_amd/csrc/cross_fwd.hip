@@ -166,25 +166,31 @@ __device__ __forceinline__ void rows_body(const Queries &a, const States &st, in
     const char *kp = (const char *)((const S *)st.k + b0 * st.lk.sb + j * st.lk.sh);
     const char *vp = (const char *)((const S *)st.v + b0 * st.lv.sb + j * st.lv.sh);
     const long long ks = st.lk.st * (long long)sizeof(S), vs = st.lv.st * (long long)sizeof(S);
-    auto fetch = [&](int i) {
+    auto fetch = [&](int i, int half) {
         const int r = i * NT;
-        char *dst = lds + ((i - n0) & 1) * 2 * TB;
+        char *dst = lds + half * 2 * TB;
         X::template stage<NT, 8>(dst, kp + r * ks, ks, len - r, wv);
         X::template stage<NT, 8>(dst + TB, vp + r * vs, vs, len - r, wv);
     };
-    if (n0 < n1) fetch(n0);
+    if (n0 < n1) fetch(n0, 0);
     wait_loads<0>();  // the queries too: no wait for them stays in the loop
-    for (int i = n0; i < n1; ++i) {
+    // one stage from half `half` of the LDS; two to a turn of the loop, so that their addresses
+    // are constants (-3 % at 2048 x 8192, d 64)
+    auto step = [&](int i, int half) {
         wait_loads<0>();
         __syncthreads();  // this stage has arrived, the one before has been read
-        if (i + 1 < n1) fetch(i + 1);
+        if (i + 1 < n1) fetch(i + 1, half ^ 1);
         const int base = i * NT + 32 * kw;
-        if (idle || base >= len) continue;
-        const char *kt = lds + ((i - n0) & 1) * 2 * TB, *vt = kt + TB;
+        if (idle || base >= len) return;
+        const char *kt = lds + half * 2 * TB, *vt = kt + TB;
         f32x16_t s = logits<S, D>(kt, 32 * kw, w);
         if (base + 32 > low) mask<S, D>(s, base, w);
         weights<S, D>(s, a.scale, w);
         values<S, D>(vt, 32 * kw, s, w);
+    };
+    for (int i = n0; i < n1; i += 2) {
+        step(i, 0);
+        if (i + 1 < n1) step(i + 1, 1);
     }
     float l = half_sum(w.l);
     if (KW > 1) {
