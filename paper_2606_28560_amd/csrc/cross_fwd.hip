@@ -31,6 +31,7 @@ template <typename S, int D> struct Rows {
     Frag<S> q[D / 16];
     f32x16_t acc[D / 32];  // transposed: column = row of the lane
     float m, l;            // running maximum (in powers of two) and the lane's own part of the sum
+    float neg, top;        // -m, or 0 while m is -inf; the logit above which m moves
     int lim;               // rows of the states that this row reads
     long long id;          // (b H + h) T + t
     RowAt at;
@@ -50,8 +51,8 @@ __device__ __forceinline__ void load_rows(const Queries &a, const States &st, in
     for (int ks = 0; ks < D / 16; ++ks) load_frag(row, ks, h, w.q[ks]);
 #pragma unroll
     for (int dt = 0; dt < D / 32; ++dt) w.acc[dt] = zero16();
-    w.m = -INFINITY;
-    w.l = 0.f;
+    w.m = w.top = -INFINITY;
+    w.l = w.neg = 0.f;
 }
 
 template <typename S, int D>
@@ -77,26 +78,27 @@ __device__ __forceinline__ void mask(f32x16_t &s, int base, const Rows<S, D> &w)
 }
 
 // Logits to weights exp2(s - m).  The reference m moves only when a logit passes it by 8
-// powers of two: the sums keep their 24 bits and the accumulators are rarely rescaled.
+// powers of two: the sums keep their 24 bits and the accumulators are rarely rescaled.  What a
+// tile has to look at is the lane's own maximum; the halves' common one is taken with the move.
 template <typename S, int D>
 __device__ __forceinline__ void weights(f32x16_t &s, float scale, Rows<S, D> &w) {
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-    top = half_max(top) * scale;
-    if (__ballot(top > w.m + 8.f)) {
-        const float m = fmaxf(top, w.m);
+    if (__ballot(top > w.top)) {
+        const float m = fmaxf(half_max(top) * scale, w.m);
         const float f = m == -INFINITY ? 1.f : ex2(w.m - m);
         w.m = m;
+        w.neg = m == -INFINITY ? 0.f : -m;
+        w.top = (m + 8.f) * __builtin_amdgcn_rcpf(scale);
         w.l *= f;
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) w.acc[dt] *= f;
     }
-    const float m = w.m == -INFINITY ? 0.f : w.m;
     float l = 0.f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-        s[i] = ex2(fmaf(s[i], scale, -m));
+        s[i] = ex2(fmaf(s[i], scale, w.neg));
         l += s[i];
     }
     w.l += l;
