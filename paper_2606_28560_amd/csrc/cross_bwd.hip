@@ -619,8 +619,9 @@ double tile_us(int dtype, int D, bool dkv) {
 // How a gradient over `rows` rows to a problem is computed: narrow workgroups (32 rows, the
 // other side's rows divided among the waves) or wide ones (128 rows), and in how many pieces
 // of the other side's `steps` rows: the least of an estimate of the time.  Wide and narrow dk,
-// dv measured: 128 and 218 microseconds at 2 x 16 heads on 4 of 1000 x 2500, d 128, bfloat16;
-// 75 and 32 at 4 x 8 heads of 200 x 200, d 128, float32.
+// dv measured, in their best pieces, without the pieces' sum: 117 and 201 microseconds at 2 x 16
+// heads on 4 of 1000 x 2500, d 128, bfloat16; 32 (two or more pieces) and 30 (one) at 4 x 8 heads
+// of 200 x 200, d 128, float32.
 void divide(int dtype, int D, long long prob, int rows, int steps, bool dkv, int *narrow, int *tiles, int *pieces) {
     const double us = tile_us(dtype, D, dkv);
     const int n = (steps + 31) / 32;

@@ -536,9 +536,10 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
 // By rows or by keys, row tiles and pieces of states for `prob` problems: the least of an
 // estimate of the time.  A wave takes 0.007 D microseconds for a tile of 32 x 32 in bfloat16,
 // 0.022 D in float32; two waves to a SIMD take 1.5 times as long as one.  By rows and by keys
-// measured: 38 and 54 microseconds at 8 x 8 heads of 1024 x 1024, d 64, bfloat16; 33 and 25
-// where 64 sequences of 16 heads on 4 share 8192 rows, d 128.  beside: how states of the same
-// call are read, whose launch these share if they are read so too (-1: none).
+// measured, each in its best pieces: 35 and 51 microseconds at 8 x 8 heads of 1024 x 1024, d 64,
+// bfloat16; 41 and 28 (both launches and the join) where 64 sequences of 16 heads on 4 share 8192
+// rows, d 128.  beside: how states of the same call are read, whose launch these share if they
+// are read so too (-1: none).
 void plan(int dtype, int D, States *s, int prob, int beside = -1) {
     const double us = (dtype == 1 ? 0.007 : 0.022) * D, row = 2.0 * D * (dtype == 1 ? 2 : 4);
     const int n = (s->S + 31) / 32;
