@@ -538,9 +538,11 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
 // 0.022 D in float32; two waves to a SIMD take 1.5 times as long as one.  By rows and by keys
 // measured, each in its best pieces: 35 and 51 microseconds at 8 x 8 heads of 1024 x 1024, d 64,
 // bfloat16; 41 and 28 (both launches and the join) where 64 sequences of 16 heads on 4 share 8192
-// rows, d 128.  beside: how states of the same call are read, whose launch these share if they
-// are read so too (-1: none).
-void plan(int dtype, int D, States *s, int prob, int beside = -1) {
+// rows, d 128.  joined: the call has a join in any case; else pieces add its launch, 5 microseconds.
+// (Against 3 in both cases, of drawn shapes for which it matters: 1.04 times as fast in a graph
+// and 1.09 from the host in 40 without, 1.02 and 1.00 in 30 with other states.)  beside: how
+// states of the same call are read, whose launch these share if they are read so too (-1: none).
+void plan(int dtype, int D, States *s, int prob, bool joined, int beside = -1) {
     const double us = (dtype == 1 ? 0.007 : 0.022) * D, row = 2.0 * D * (dtype == 1 ? 2 : 4);
     const int n = (s->S + 31) / 32;
     double best = 1e30;
@@ -558,7 +560,7 @@ void plan(int dtype, int D, States *s, int prob, int beside = -1) {
             const double read = (once > all ? once : all) / busy + 3.0;
             if (read > x) x = read;
             if (beside >= 0 && rw != beside) x += 4.0;
-            if (p > 1) x += 3.0 + p * (double)prob * s->rows * D * 8e-6 / 3.0;
+            if (p > 1) x += (joined ? 1.5 : 5.0) + p * (double)prob * s->rows * D * 8e-6 / 3.0;
             if (x < best) {
                 best = x;
                 s->rw = rw;
@@ -619,8 +621,8 @@ template <typename S> hipError_t join_d(int D, const JoinArgs &a, hipStream_t st
 }  // namespace
 
 int plan_cross_forward(int dtype, int D, States *s0, States *s1, int prob0, int prob1) {
-    if (s1) plan(dtype, D, s1, prob1);
-    plan(dtype, D, s0, prob0, s1 ? s1->rw : -1);
+    if (s1) plan(dtype, D, s1, prob1, true);
+    plan(dtype, D, s0, prob0, s1 != nullptr, s1 ? s1->rw : -1);
     s0->slot = 0;
     if (!s1) return s0->splits;
     s1->slot = s0->splits;
