@@ -118,7 +118,8 @@ size_t fibattn_backward_workspace_bytes(int B, int H, int T, int d_head, int W, 
  *   dO   : upstream gradient of o, dtype, [B,H,T,d_head]
  *   dq, dk, dv : gradients (written), dtype; accumulated in float32, rounded once
  *   dalpha : device float32 (overwritten): sum over b, h, i and rung entries of
- *            f_k * dL/dw_k (dw_k/dalpha = f_k); reduced in float64 in fixed order
+ *            f_k * dL/dw_k (dw_k/dalpha = f_k); reduced in float64 in fixed order.  Not
+ *            the gradient where o and lse are joined ones: fibattn_backward_joined
  *   workspace : device buffer of at least fibattn_backward_workspace_bytes(...)
  *   rope_base : 0 -> dq, dk are gradients w.r.t. the rotated q, k passed in;
  *               > 1 -> the inverse rotation R^T at true positions (same pairing and
@@ -287,6 +288,28 @@ fibattn_status_t fibattn_backward_dt(const void *q, const void *k, const void *v
                                      const void *table, float rope_base,
                                      fibattn_dtype_t dtype, hipStream_t stream);
 
+/*
+ * The backward of a layer whose entries are a part of the softmax of lse and o: its output
+ * was joined with attention to other rows (fibattn_join), and lse and o are the joined ones.
+ * The other backward calls give the same dq, dk and dv there, but their dalpha (and dtheta)
+ * takes Delta_i from the layer's own entries, which is <dO_i, o_i> only where these are the
+ * whole softmax: with a joined lse and o it is not the gradient.  Here it is, with
+ * Delta_i = <dO_i, o_i> of the stored o (whose rounding it then has).
+ *   layouts : as fibattn_backward_strided, or NULL: packed
+ *   table   : a device table, as fibattn_backward_dt (base, K and alpha are not used, layouts
+ *             must be NULL, the workspace is that of K = 0), or NULL: base, K and alpha, and
+ *             dtheta must be NULL
+ * Everything else as fibattn_backward_gqa.
+ */
+fibattn_status_t fibattn_backward_joined(const void *q, const void *k, const void *v,
+                                         const void *o, const float *lse, const void *dO,
+                                         void *dq, void *dk, void *dv, float *dalpha, float *dtheta,
+                                         void *workspace, size_t workspace_bytes,
+                                         const fibattn_layout_t *layouts,
+                                         int B, int H, int H_kv, int T, int d_head, int W,
+                                         const int32_t *base, int K, float alpha, const void *table,
+                                         float rope_base, fibattn_dtype_t dtype, hipStream_t stream);
+
 fibattn_status_t fibattn_device_table_theta(const float *theta, float *alpha,
                                             const int32_t *base, int K, int W,
                                             void *table, hipStream_t stream);
@@ -431,6 +454,8 @@ fibattn_status_t fibattn_prefix_forward(const void *q, const void *k_prefix, con
  * o = exp(lse_a - lse) o_a + exp(lse_b - lse) o_b.  A part whose lse is -inf counts nothing
  * whatever its o holds; with both so, o is 0 and lse -inf.  o and lse may be o_a and lse_a,
  * or o_b and lse_b.  layouts: o_a, o_b, o, or NULL: packed [B, H, T, d_head].
+ * Gradients: each part's backward with the joined o and lse gives its own; a sparse layer's
+ * dalpha and dtheta come from fibattn_backward_joined alone.
  */
 fibattn_status_t fibattn_join(const void *o_a, const float *lse_a, const void *o_b, const float *lse_b,
                               void *o, float *lse, const fibattn_layout_t *layouts, int B, int H, int T,

@@ -281,7 +281,7 @@ static fibattn_status_t backward_impl(const void *q, const void *k, const void *
                                       size_t workspace_bytes, const Layouts &lay, int B, int H,
                                       int H_kv, int T, int d_head, int W, const int32_t *base,
                                       int K, float alpha, float rope_base, fibattn_dtype_t dtype,
-                                      hipStream_t stream) {
+                                      hipStream_t stream, bool joined = false) {
     fibattn_status_t st = check_common(B, H, T, d_head, W, K, dtype);
     if (st != FIBATTN_OK) return st;
     if (H_kv < 1 || H_kv > H || H % H_kv != 0) return FIBATTN_ERR_INVALID_ARG;
@@ -298,11 +298,11 @@ static fibattn_status_t backward_impl(const void *q, const void *k, const void *
     if (st != FIBATTN_OK) return st;
     float *delta_ws = (float *)workspace;
     double *partials = (double *)((char *)workspace + wl.partials);
-    const RungTerms terms{(uint32_t *)((char *)workspace + wl.terms), wl.planes};
+    const RungTerms terms{(uint32_t *)((char *)workspace + wl.terms), (int16_t)wl.planes, 0};
     const RopeFreq rf = make_rope_freq((double)rope_base, d_head);
     const Heads hd{H, H / H_kv};
     hipError_t e = launch_backward((int)dtype, d_head, q, k, v, o, lse, dO, dq, dk, dv, dalpha, nullptr,
-                                   delta_ws, partials, terms, B * H, hd, T, W, rt, nullptr, rf, lay, stream);
+                                   delta_ws, partials, terms, B * H, hd, T, W, rt, nullptr, rf, lay, joined, stream);
     return e == hipSuccess ? FIBATTN_OK : FIBATTN_ERR_HIP;
 }
 
@@ -318,6 +318,17 @@ fibattn_status_t fibattn_backward_gqa(const void *q, const void *k, const void *
                          rope_base, dtype, stream);
 }
 
+// The eight placements of a backward.
+static fibattn_status_t backward_layouts(const fibattn_layout_t *layouts, int T, int d_head, fibattn_dtype_t dtype,
+                                         Layouts *lay) {
+    Layout *dst[8] = {&lay->q, &lay->k, &lay->v, &lay->o, &lay->g, &lay->dq, &lay->dk, &lay->dv};
+    for (int a = 0; a < 8; ++a) {
+        const fibattn_status_t st = check_layout(layouts[a], T, d_head, dtype, dst[a]);
+        if (st != FIBATTN_OK) return st;
+    }
+    return FIBATTN_OK;
+}
+
 fibattn_status_t fibattn_backward_strided(const void *q, const void *k, const void *v, const void *o,
                                           const float *lse, const void *dO, void *dq, void *dk,
                                           void *dv, float *dalpha, void *workspace,
@@ -327,11 +338,8 @@ fibattn_status_t fibattn_backward_strided(const void *q, const void *k, const vo
                                           fibattn_dtype_t dtype, hipStream_t stream) {
     if (!layouts || T < 1) return FIBATTN_ERR_INVALID_ARG;
     Layouts lay = packed_layouts(H, H_kv > 0 ? H_kv : 1, T, d_head);
-    Layout *dst[8] = {&lay.q, &lay.k, &lay.v, &lay.o, &lay.g, &lay.dq, &lay.dk, &lay.dv};
-    for (int a = 0; a < 8; ++a) {
-        const fibattn_status_t st = check_layout(layouts[a], T, d_head, dtype, dst[a]);
-        if (st != FIBATTN_OK) return st;
-    }
+    const fibattn_status_t st = backward_layouts(layouts, T, d_head, dtype, &lay);
+    if (st != FIBATTN_OK) return st;
     return backward_impl(q, k, v, o, lse, dO, dq, dk, dv, dalpha, workspace, workspace_bytes, lay, B, H,
                          H_kv, T, d_head, W, base, K, alpha, rope_base, dtype, stream);
 }
@@ -428,11 +436,11 @@ fibattn_status_t fibattn_forward_rope_q_dt(const void *q, const void *k, const v
                                stream);
 }
 
-fibattn_status_t fibattn_backward_dt(const void *q, const void *k, const void *v, const void *o,
-                                     const float *lse, const void *dO, void *dq, void *dk, void *dv,
-                                     float *dalpha, float *dtheta, void *workspace, size_t workspace_bytes, int B,
-                                     int H, int H_kv, int T, int d_head, int W, const void *table,
-                                     float rope_base, fibattn_dtype_t dtype, hipStream_t stream) {
+static fibattn_status_t backward_dt_impl(const void *q, const void *k, const void *v, const void *o,
+                                         const float *lse, const void *dO, void *dq, void *dk, void *dv,
+                                         float *dalpha, float *dtheta, void *workspace, size_t workspace_bytes, int B,
+                                         int H, int H_kv, int T, int d_head, int W, const void *table,
+                                         float rope_base, fibattn_dtype_t dtype, hipStream_t stream, bool joined) {
     fibattn_status_t st = check_common(B, H, T, d_head, W, 0, dtype);
     if (st != FIBATTN_OK) return st;
     if (H_kv < 1 || H_kv > H || H % H_kv != 0) return FIBATTN_ERR_INVALID_ARG;
@@ -448,13 +456,46 @@ fibattn_status_t fibattn_backward_dt(const void *q, const void *k, const void *v
     memset(&unused, 0, sizeof(unused));
     float *delta_ws = (float *)workspace;
     double *partials = (double *)((char *)workspace + wl.partials);
-    const RungTerms terms{(uint32_t *)((char *)workspace + wl.terms), wl.planes};
+    const RungTerms terms{(uint32_t *)((char *)workspace + wl.terms), (int16_t)wl.planes, 0};
     const RopeFreq rf = make_rope_freq((double)rope_base, d_head);
     const Heads hd{H, H / H_kv};
     hipError_t e = launch_backward((int)dtype, d_head, q, k, v, o, lse, dO, dq, dk, dv, dalpha, dtheta,
                                    delta_ws, partials, terms, B * H, hd, T, W, unused,
-                                   (const RungTable *)table, rf, packed_layouts(H, H_kv, T, d_head), stream);
+                                   (const RungTable *)table, rf, packed_layouts(H, H_kv, T, d_head), joined, stream);
     return e == hipSuccess ? FIBATTN_OK : FIBATTN_ERR_HIP;
+}
+
+fibattn_status_t fibattn_backward_dt(const void *q, const void *k, const void *v, const void *o,
+                                     const float *lse, const void *dO, void *dq, void *dk, void *dv,
+                                     float *dalpha, float *dtheta, void *workspace, size_t workspace_bytes, int B,
+                                     int H, int H_kv, int T, int d_head, int W, const void *table,
+                                     float rope_base, fibattn_dtype_t dtype, hipStream_t stream) {
+    return backward_dt_impl(q, k, v, o, lse, dO, dq, dk, dv, dalpha, dtheta, workspace, workspace_bytes, B, H, H_kv, T,
+                            d_head, W, table, rope_base, dtype, stream, false);
+}
+
+fibattn_status_t fibattn_backward_joined(const void *q, const void *k, const void *v, const void *o,
+                                         const float *lse, const void *dO, void *dq, void *dk, void *dv,
+                                         float *dalpha, float *dtheta, void *workspace, size_t workspace_bytes,
+                                         const fibattn_layout_t *layouts, int B, int H, int H_kv, int T, int d_head,
+                                         int W, const int32_t *base, int K, float alpha, const void *table,
+                                         float rope_base, fibattn_dtype_t dtype, hipStream_t stream) {
+    if (table) {
+        if (layouts) return FIBATTN_ERR_INVALID_ARG;  // device tables come with packed tensors
+        return backward_dt_impl(q, k, v, o, lse, dO, dq, dk, dv, dalpha, dtheta, workspace, workspace_bytes, B, H,
+                                H_kv, T, d_head, W, table, rope_base, dtype, stream, true);
+    }
+    if (dtheta) return FIBATTN_ERR_INVALID_ARG;  // a host alpha has no theta
+    fibattn_status_t st = check_common(B, H, T, d_head, W, K, dtype);
+    if (st != FIBATTN_OK) return st;
+    if (H_kv < 1 || H_kv > H || H % H_kv != 0) return FIBATTN_ERR_INVALID_ARG;
+    Layouts lay = packed_layouts(H, H_kv, T, d_head);
+    if (layouts) {
+        st = backward_layouts(layouts, T, d_head, dtype, &lay);
+        if (st != FIBATTN_OK) return st;
+    }
+    return backward_impl(q, k, v, o, lse, dO, dq, dk, dv, dalpha, workspace, workspace_bytes, lay, B, H, H_kv, T,
+                         d_head, W, base, K, alpha, rope_base, dtype, stream, true);
 }
 
 fibattn_status_t fibattn_alpha_from_theta(const float *theta, float *alpha, int n, hipStream_t stream) {

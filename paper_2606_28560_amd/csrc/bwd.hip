@@ -17,7 +17,8 @@
 // to the storage type) but from the entries themselves, Delta_i = sum_e p_e dP_e (the
 // same quantity, since o_i = sum_e p_e vhat_e): per query it accumulates
 // Xa = sum f p dP <q, k[r1]-k[r0]>, Xb = sum f p <dO, v[r1]-v[r0]>, Y = sum f p <q, k[r1]-k[r0]>
-// and the entries' sum of p dP, and adds tau (Xa - Delta Y) + Xb.
+// and the entries' sum of p dP, and adds tau (Xa - Delta Y) + Xb.  Where the entries are a
+// part of the softmax of lse and o (joined), their sum is not Delta: there it is <dO_i, o_i>.
 //
 // Because every rung offset is shared, the queries that read key row j are again a
 // fixed set of shifted positions: j .. j+W through the window, and j + floor(d_k)
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(256, (dq_waves<D>)) void bwd_dq_tile_kernel(
     const uint16_t *__restrict__ o, const float *__restrict__ lse, const uint16_t *__restrict__ dO,
     uint16_t *__restrict__ dq, float *__restrict__ delta_out, double *__restrict__ partials, int T,
     int W, RungTable rt_arg, const RungTable *__restrict__ rtp, RopeFreq rf, float tau, float sl2, TileShape ts, Heads hd,
-    Layouts lay) {
+    Layouts lay, int joined) {
     using S = uint16_t;
     using TL = Tile<S, D>;
     using Slice = typename TL::Slice;
@@ -282,7 +283,7 @@ __global__ __launch_bounds__(256, (dq_waves<D>)) void bwd_dq_tile_kernel(
         if (gq == 0) delta_out[(size_t)bh * T + i] = bad ? NAN : delta;
     }
     // this lane's part of the query's dalpha; wave sums, then the waves in order
-    double dal = i < T ? (double)tau * (xa - dsum * y) + xb : 0.0;
+    double dal = i < T ? (double)tau * (xa - (joined ? (double)delta : dsum) * y) + xb : 0.0;
     if (bad) dal = NAN;
 #pragma unroll
     for (int st = 32; st >= 1; st >>= 1) dal += __shfl_xor(dal, st, 64);
@@ -308,7 +309,7 @@ __global__ __launch_bounds__(256, 2) void bwd_dq_f32_kernel(
     const float *__restrict__ o, const float *__restrict__ lse, const float *__restrict__ dO,
     float *__restrict__ dq, float *__restrict__ delta_out, double *__restrict__ partials, int T, int W,
     RungTable rt_arg, const RungTable *__restrict__ rtp, RopeFreq rf, float tau, int tiles, int blocks, int rows,
-    Heads hd, Layouts lay) {
+    Heads hd, Layouts lay, int joined) {
     using TL = Tile<float, D, L>;
     using Slice = typename TL::Slice;
     const RungTable &rt = DEV ? *rtp : rt_arg;
@@ -407,7 +408,7 @@ __global__ __launch_bounds__(256, 2) void bwd_dq_f32_kernel(
     }
     if (__builtin_amdgcn_ballot_w64(!(TL::finite(acc) && (xa + xb + y + dsum) * 0.0 == 0.0)))
         dq_by_entry<TL>(qq, gg, K, V, sk, sv, ic, gq, W, rt, nact, tau, sl2, lse2, delta, acc, xa, xb, y, dsum);
-    double dal = gq == 0 && i < T ? (double)tau * (xa - dsum * y) + xb : 0.0;
+    double dal = gq == 0 && i < T ? (double)tau * (xa - (joined ? (double)delta : dsum) * y) + xb : 0.0;
     if (bad) dal = NAN;
     if (rf.on) TL::rope_t(acc, i, sfreq, gq);  // gradient w.r.t. the unrotated q
     if (i < T) {
@@ -964,7 +965,8 @@ static hipError_t launch_bwd_t(const void *q, const void *k, const void *v, cons
                                const float *lse, const void *dO, void *dq, void *dk, void *dv,
                                float *dalpha, float *dtheta, float *delta_ws, double *partials, int BH,
                                const Heads &hd, int T, int W, const RungTable &rt,
-                               const RungTable *rtp, const RopeFreq &rf, const Layouts &lay, hipStream_t s) {
+                               const RungTable *rtp, const RopeFreq &rf, const Layouts &lay, bool joined,
+                               hipStream_t s) {
     using TL = Tile<S, D>;
     constexpr int nw = TL::kRow == 512 ? 2 : 4;  // waves per workgroup (float32 d 128: its rows' LDS)
     const float tau = 1.f / sqrtf((float)D);
@@ -991,13 +993,13 @@ static hipError_t launch_bwd_t(const void *q, const void *k, const void *v, cons
                         : (rtp ? bwd_dq_f32_kernel<D, 4, true> : bwd_dq_f32_kernel<D, 4, false>);
         e = launch(kBwdDq, dqk, grid_of(nb), dim3(256), (unsigned)(2 * rows * TL::kRow), s, (const S *)q,
                    (const S *)k, (const S *)v, (const S *)o, lse, (const S *)dO, (S *)dq, delta_ws, partials, T, W, rt,
-                   rtp, rf, tau, tiles, nb, rows, hd, lay);
+                   rtp, rf, tau, tiles, nb, rows, hd, lay, (int)joined);
     } else {
         auto dqk = rtp ? bwd_dq_tile_kernel<D, true, true>
                        : interp ? bwd_dq_tile_kernel<D, true, false> : bwd_dq_tile_kernel<D, false, false>;
         e = launch(kBwdDq, dqk, grid_of(nb), dim3(64 * nw), (unsigned)(fixed + per * ts.cps), s, (const S *)q,
                    (const S *)k, (const S *)v, (const S *)o, lse, (const S *)dO, (S *)dq, delta_ws, partials, T, W,
-                   rt, rtp, rf, tau, kLog2e / sqrtf((float)D), ts, hd, lay);
+                   rt, rtp, rf, tau, kLog2e / sqrtf((float)D), ts, hd, lay, (int)joined);
     }
     if (e != hipSuccess) return e;
     // dk, dv of few rows: one key per lanes of one 16-byte chunk, unless the tile kernel has
@@ -1041,10 +1043,10 @@ static hipError_t launch_backward_rows(int dtype, int D, const void *q, const vo
                                           void *dk, void *dv, float *dalpha, float *dtheta, float *delta_ws,
                                           double *partials, int BH, const Heads &hd, int T, int W,
                                           const RungTable &rt, const RungTable *rtp, const RopeFreq &rf,
-                                          const Layouts &lay, hipStream_t s) {
+                                          const Layouts &lay, bool joined, hipStream_t s) {
 #define FIBATTN_BWD(S_, D_)                                                                  \
     return launch_bwd_t<S_, D_>(q, k, v, o, lse, dO, dq, dk, dv, dalpha, dtheta, delta_ws, partials, \
-                                BH, hd, T, W, rt, rtp, rf, lay, s)
+                                BH, hd, T, W, rt, rtp, rf, lay, joined, s)
     if (dtype == 0 && D == 32) FIBATTN_BWD(float, 32);
     if (dtype == 0 && D == 64) FIBATTN_BWD(float, 64);
     if (dtype == 1 && D == 32) FIBATTN_BWD(uint16_t, 32);
@@ -1060,12 +1062,12 @@ hipError_t launch_backward(int dtype, int D, const void *q, const void *k, const
                            void *dv, float *dalpha, float *dtheta, float *delta_ws, double *partials,
                            const RungTerms &terms, int BH, const Heads &hd, int T, int W,
                            const RungTable &rt, const RungTable *rtp, const RopeFreq &rf,
-                           const Layouts &lay, hipStream_t s) {
+                           const Layouts &lay, bool joined, hipStream_t s) {
     if (backward_mfma_supported(dtype, D, W))
         return launch_backward_mfma(q, k, v, o, lse, dO, dq, dk, dv, dalpha, dtheta, delta_ws, partials,
-                                    terms, BH, hd, T, W, rt, rtp, rf, lay, s);
+                                    RungTerms{terms.p, terms.planes, (int16_t)joined}, BH, hd, T, W, rt, rtp, rf, lay, s);
     return launch_backward_rows(dtype, D, q, k, v, o, lse, dO, dq, dk, dv, dalpha, dtheta, delta_ws,
-                                   partials, BH, hd, T, W, rt, rtp, rf, lay, s);
+                                   partials, BH, hd, T, W, rt, rtp, rf, lay, joined, s);
 }
 
 }  // namespace fibattn

@@ -14,7 +14,8 @@
 //          dq += tau dS ((1-w) k[r0] + w k[r1]) on the VALU,
 //          dalpha partial += f (tau dS <q, k[r1]-k[r0]> + p <dO, v[r1]-v[r0]>), where
 //          the dS of this sum uses Delta_i = sum_e p_e dP_e over the query's entries
-//          rather than the one from the stored (bf16) o;
+//          rather than the one from the stored (bf16) o, unless the entries are a part of
+//          the softmax;
 //   writes dq, Delta_i = <dO_i, o_i>, one float64 dalpha partial per workgroup
 //   (each query's terms in float32, then float64 across queries) and, for every rung
 //   entry, the pair (tau dS, p) as bfloat16 (the rung terms, staged in LDS during the
@@ -196,7 +197,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void b
     // to bf16) but the entries' own Delta_i = sum_e p_e dP_e, known after the loop: the
     // lane accumulates xa = sum f p dP ds, xb = sum f p dv and y = sum f p ds over its
     // parts ds of <q, k[r1]-k[r0]> and dv of <dO, v[r1]-v[r0]>, and its dalpha terms are
-    // tau (xa - Delta y) + xb (float32 per lane; float64 across lanes below).
+    // tau (xa - Delta y) + xb (float32 per lane; float64 across lanes below).  Where the entries
+    // are a part of the softmax (joined) their sum is a part of Delta, which then is the o's.
     float xa = 0.f, xb = 0.f, y = 0.f;
     auto compute_rung = [&](int r, const Slice *x) {  // x = {k0, v0, k1, v1}
         const int d0 = rt.d0[r];
@@ -259,7 +261,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(4))) void b
         store_acc(dq + head_at<STRIDED, kD>(lay.dq, bh, hd.H, T) + (size_t)i * stdq, gq, acc, bad ? NAN : 1.f);
         if (gq == 0) delta_out[(size_t)bh * T + i] = bad ? NAN : delta;
     }
-    float dal_q = fmaf(tau, fmaf(-dsum, y, xa), xb);
+    float dal_q = fmaf(tau, fmaf(-(terms.joined ? delta : dsum), y, xa), xb);
     if (bad) dal_q = NAN;
     // workgroup dalpha partial: wave sums, then the four waves in order
     double dal = (double)dal_q;

@@ -95,10 +95,12 @@ struct TableJob {
 // hands to its dk/dv kernel: for query i of flat head bh and rung r of the table, the
 // bfloat16 pair (tau dS, p) (tau dS in the low half) at index (bh * planes + r) * T + i
 // (planes >= the table's n).  The dk/dv accumulation rounds these weights to bfloat16
-// anyway.
+// anyway.  joined: the entries are a part of the softmax of lse and o (for dalpha); in one word
+// with planes, which the dq kernel holds to its end anyway (as an argument of its own it made
+// the kernels of device tables spill 52 scalar registers for 31: 55.3 for 54.6 us at B32 H8 T1024).
 struct RungTerms {
     uint32_t *p;
-    int planes;
+    int16_t planes, joined;
 };
 
 // Grouped key/value heads (Section 3 "Model and training": 8 query heads share 2

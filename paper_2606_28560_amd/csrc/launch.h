@@ -66,13 +66,15 @@ inline bool f32_wide(int BH, int T) { return (long long)BH * T <= 12288; }
 // dalpha partials the workspace holds: at least one per workgroup of the dq kernel.
 size_t bwd_num_partials(int dtype, int D, int BH, int T);
 
-// dtheta (nullable, device tables only): also writes dalpha * rtp->dadtheta there.
+// dtheta (nullable, device tables only): also writes dalpha * rtp->dadtheta there.  joined:
+// the entries are a part of the softmax of lse and o (dalpha takes Delta from o); in terms for
+// launch_backward_mfma.
 hipError_t launch_backward(int dtype, int D, const void *q, const void *k, const void *v,
                            const void *o, const float *lse, const void *dO, void *dq, void *dk,
                            void *dv, float *dalpha, float *dtheta, float *delta_ws, double *partials,
                            const RungTerms &terms, int BH, const Heads &hd, int T, int W,
                            const RungTable &rt, const RungTable *rtp, const RopeFreq &rf,
-                           const Layouts &lay, hipStream_t s);
+                           const Layouts &lay, bool joined, hipStream_t s);
 
 // bfloat16, d_head = 64, W <= 16: matrix-core band + VALU rungs (fwd_mfma.hip, bwd_mfma.hip).
 bool forward_mfma_supported(int dtype, int D, int W);

@@ -32,6 +32,7 @@ EXPORTED = ("fibattn_rung_table", "fibattn_forward", "fibattn_backward_workspace
             "fibattn_rope_qk", "fibattn_status_string", "fibattn_timing_begin", "fibattn_timing_end",
             "fibattn_backward_noalloc", "fibattn_device_table_theta", "fibattn_rope_qk_table",
             "fibattn_forward_rope_q", "fibattn_forward_rope_q_dt", "fibattn_forward_rope_q_strided",
+            "fibattn_backward_joined",
             "fibattn_cross_workspace_bytes", "fibattn_cross_forward", "fibattn_cross_backward_workspace_bytes",
             "fibattn_cross_backward", "fibattn_prefix_workspace_bytes", "fibattn_prefix_forward", "fibattn_join")
 SCRATCH_BYTES = 64 << 20  # FIBATTN_SCRATCH_BYTES: the allocation-free backward's static scratch
@@ -107,6 +108,8 @@ def lib():
     L.fibattn_backward_noalloc.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                            i, i, i, i, i, i, ip, i, f, f, i, vp]
     L.fibattn_backward_noalloc.restype = i
+    L.fibattn_backward_joined.argtypes = [vp] * 12 + [sz, vp] + [i] * 6 + [ip, i, f, vp, f, i, vp]
+    L.fibattn_backward_joined.restype = i
     L.fibattn_cross_workspace_bytes.argtypes = [i] * 7
     L.fibattn_cross_workspace_bytes.restype = sz
     L.fibattn_cross_forward.argtypes = [vp] * 7 + [sz, vp] + [i] * 8 + [vp]
@@ -332,8 +335,11 @@ def fibattn_backward_workspace_bytes(B: int, H: int, T: int, d_head: int, W: int
 
 
 def fibattn_backward(q, k, v, o, lse, dO, W: int, base, alpha: float, *, dq=None, dk=None, dv=None,
-                     dalpha=None, workspace=None, rope_base: float = 0.0, stream=None):
+                     dalpha=None, workspace=None, rope_base: float = 0.0, joined=False, stream=None):
     """dq, dk, dv, dalpha (a 1-element float32 device tensor).
+
+    joined: o and lse are joined ones (fibattn_join) of which this layer is a part; without it
+    dalpha is not the gradient there (dq, dk, dv are the same).
 
     k, v (and dk, dv) may have fewer heads than q (grouped heads; dk, dv then sum over
     each group).  rope_base > 0: dq, dk are returned w.r.t. the unrotated q, k (R^T
@@ -364,7 +370,13 @@ def fibattn_backward(q, k, v, o, lse, dO, W: int, base, alpha: float, *, dq=None
             workspace.numel())
     tail = (T, D, int(W), bp, len(b), ctypes.c_float(alpha), ctypes.c_float(rope_base),
             _dtype_code(q), _stream(stream))
-    if not _packed(q, k, v, o, dO, dq, dk, dv):
+    if joined:
+        lay = None if _packed(q, k, v, o, dO, dq, dk, dv) else _layouts(q, k, v, o, dO, dq, dk, dv)
+        st = lib().fibattn_backward_joined(*ptrs[:10], None, *ptrs[10:], lay, B, H, Hkv, T, D, int(W), bp, len(b),
+                                           ctypes.c_float(alpha), None, ctypes.c_float(rope_base), _dtype_code(q),
+                                           _stream(stream))
+        _check("fibattn_backward_joined", st)
+    elif not _packed(q, k, v, o, dO, dq, dk, dv):
         st = lib().fibattn_backward_strided(*ptrs, _layouts(q, k, v, o, dO, dq, dk, dv), B, H, Hkv, *tail)
         _check("fibattn_backward_strided", st)
     elif Hkv == H:
@@ -464,7 +476,7 @@ def fibattn_forward_dt(q, k, v, W: int, table, *, o=None, lse=None, stream=None)
 
 
 def fibattn_backward_dt(q, k, v, o, lse, dO, W: int, table, *, dq=None, dk=None, dv=None,
-                        dalpha=None, dtheta=None, workspace=None, rope_base: float = 0.0, stream=None):
+                        dalpha=None, dtheta=None, workspace=None, rope_base: float = 0.0, joined=False, stream=None):
     """As fibattn_backward, with the rung table built on the device; with `dtheta` (a
     float32 device tensor) and a table built from theta, also dL/dtheta."""
     import torch
@@ -486,13 +498,16 @@ def fibattn_backward_dt(q, k, v, o, lse, dO, W: int, table, *, dq=None, dk=None,
     need = fibattn_backward_workspace_bytes(B, H, T, D, W, 0)
     if workspace is None:
         workspace = torch.empty(max(need, 1), device=q.device, dtype=torch.uint8)
-    st = lib().fibattn_backward_dt(q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
-                                   dO.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                   dalpha.data_ptr(), None if dtheta is None else dtheta.data_ptr(),
-                                   workspace.data_ptr(), workspace.numel(),
-                                   B, H, Hkv, T, D, int(W), table.data_ptr(), ctypes.c_float(rope_base),
-                                   _dtype_code(q), _stream(stream))
-    _check("fibattn_backward_dt", st)
+    ptrs = (q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), dO.data_ptr(), dq.data_ptr(),
+            dk.data_ptr(), dv.data_ptr(), dalpha.data_ptr(), None if dtheta is None else dtheta.data_ptr(),
+            workspace.data_ptr(), workspace.numel())
+    tail = (table.data_ptr(), ctypes.c_float(rope_base), _dtype_code(q), _stream(stream))
+    if joined:
+        st = lib().fibattn_backward_joined(*ptrs, None, B, H, Hkv, T, D, int(W), None, 0, ctypes.c_float(0.0), *tail)
+        _check("fibattn_backward_joined", st)
+    else:
+        st = lib().fibattn_backward_dt(*ptrs, B, H, Hkv, T, D, int(W), *tail)
+        _check("fibattn_backward_dt", st)
     return dq, dk, dv, dalpha
 
 
@@ -815,7 +830,7 @@ def fibattn_join(o_a, lse_a, o_b, lse_b, *, o=None, lse=None, stream=None):
     part whose lse is -inf counts nothing.  o and lse may be o_a and lse_a or o_b and lse_b.
 
     The backward of each part with the joined o and lse gives that part's gradients: dq is
-    the sum of the parts' dq (dalpha alone is not defined by one part's rows)."""
+    the sum of the parts' dq; a sparse layer's dalpha needs fibattn_backward(joined=True)."""
     dev = o_a.get_device()
     ctx = _elsewhere(o_a, dev, stream)
     if ctx is not None:
