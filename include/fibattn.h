@@ -415,7 +415,9 @@ fibattn_status_t fibattn_cross_forward(const void *q, const void *k, const void 
  * Its gradients: dq like q; dk, dv like k, summed over the query heads and, with B_kv = 1,
  * over the batch (0 behind the lengths).  The weights are exp(tau <q, k_j> - lse) and the
  * rows' <dO, o> is taken from o: lse and o may be those of a softmax over more than these
- * states (fibattn_join); the gradients are then this part's share of it.
+ * states (fibattn_join); the gradients are then this part's share of it.  A weight has the
+ * rounding of lse in it, 2^-23 |lse| of it: gradients lose their digits as |lse| grows, and
+ * past 2^23 they have none (the forward is right for any finite logits).
  * layouts: q, k, v, o, dO, dq, dk, dv, or NULL: packed.  workspace:
  * fibattn_cross_backward_workspace_bytes(...) bytes, never 0 for sizes in the limits.
  */

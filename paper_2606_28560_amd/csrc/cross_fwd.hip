@@ -77,20 +77,29 @@ __device__ __forceinline__ void mask(f32x16_t &s, int base, const Rows<S, D> &w)
         if (base + 8 * (i >> 2) + 4 * h + (i & 3) >= w.lim) s[i] = -INFINITY;
 }
 
+// A reference m from here on is rounded by up to 16 powers of two and more: a weight
+// exp2(s scale - m), whose product is not rounded, may be 0 for the largest logit too, and the
+// row is done again (again()).
+__device__ __forceinline__ bool coarse(float m) { return fabsf(m) >= 0x1p28f && fabsf(m) < INFINITY; }
+
 // Logits to weights exp2(s - m).  The reference m moves only when a logit passes it by 8
 // powers of two: the sums keep their 24 bits and the accumulators are rarely rescaled.  What a
 // tile has to look at is the lane's own maximum; the halves' common one is taken with the move.
+// A coarse m is a step up, so that no weight passes 1, and moves with every tile: sums that
+// are not used in the end (a larger m follows, or the row is done again) stay finite.
 template <typename S, int D>
 __device__ __forceinline__ void weights(f32x16_t &s, float scale, Rows<S, D> &w) {
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     if (__ballot(top > w.top)) {
-        const float m = fmaxf(half_max(top) * scale, w.m);
+        float m = half_max(top) * scale;
+        if (coarse(m)) m = fmaf(fabsf(m), 0x1p-23f, m);
+        m = fmaxf(m, w.m);
         const float f = m == -INFINITY ? 1.f : ex2(w.m - m);
         w.m = m;
         w.neg = m == -INFINITY ? 0.f : -m;
-        w.top = (m + 8.f) * __builtin_amdgcn_rcpf(scale);
+        w.top = coarse(m) ? -INFINITY : (m + 8.f) * __builtin_amdgcn_rcpf(scale);
         w.l *= f;
 #pragma unroll
         for (int dt = 0; dt < D / 32; ++dt) w.acc[dt] *= f;
@@ -142,9 +151,10 @@ struct Redo {
 };
 // Whether a row's sum is one that the tiles may have made not finite: of the weights l, some of
 // its values' sums are not.  (A bfloat16 row whose weights are NaN met a NaN among what it reads;
-// a float32 one may have met an infinity, of which the parts of a value make a NaN.)
-template <typename S> __device__ __forceinline__ bool again(float values, float l) {
-    return !(fabsf(values) < INFINITY) && (sizeof(S) == 4 || l == l);
+// a float32 one may have met an infinity, of which the parts of a value make a NaN.)  Or one
+// whose reference m is coarse, so that its weights may all be 0.
+template <typename S> __device__ __forceinline__ bool again(float values, float l, float m) {
+    return coarse(m) || (!(fabsf(values) < INFINITY) && (sizeof(S) == 4 || l == l));
 }
 
 // 32 RW query rows, 32 to a wave; the waves share the staged rows of the states.
@@ -236,7 +246,7 @@ __device__ __forceinline__ void rows_body(const Queries &a, const States &st, in
     for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
         for (int e = 0; e < 16; ++e) odd = fmaf(w.acc[dt][e], 0.f, odd);
-    const unsigned long long bad = __ballot(w.on && again<S>(odd, l));
+    const unsigned long long bad = __ballot(w.on && again<S>(odd, l, w.m));
     if (bad) todo = {(uint32_t)(bad | bad >> 32), b0, j, r0, n0 * NT, min(n1 * NT, len), len, slot};
     if (!w.on || (todo.which >> (lane & 31) & 1)) return;
     if (h == 0) put_lse(a, slot, w.id, w.m, l);
@@ -317,7 +327,7 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
             sum += stat[1][x][r] * f;
             y[e] += *reinterpret_cast<const f32x4_t *>(part + (32 * x + r) * D + d) * f;
         }
-        if (again<S>((y[e][0] + y[e][1]) * 0.f + (y[e][2] + y[e][3]) * 0.f, sum)) atomicOr(&odd_rows, 1u << r);
+        if (again<S>((y[e][0] + y[e][1]) * 0.f + (y[e][2] + y[e][3]) * 0.f, sum, m)) atomicOr(&odd_rows, 1u << r);
         y[e] *= sum == 0.f ? 0.f : 1.f / sum;
         lse[e] = sum == 0.f ? -INFINITY : (m + __log2f(sum)) * kLn2;
     }
@@ -357,7 +367,8 @@ __device__ __forceinline__ void put_value(float *p, float x) { *p = x; }
 //
 // The tiles multiply what a query does not read by a weight of 0, and the rest of a weight may
 // be 0 or negative: with an infinity or NaN among the values either makes a NaN of what is not
-// one.  Here nothing unread enters, and every weight is whole.
+// one.  Here nothing unread enters, every weight is whole, and a logit is rounded before the
+// largest one is subtracted from it, whose weight then is 1.
 template <typename S, int D>
 __device__ __forceinline__ void plain_rows(const Queries &a, const States &st, const Redo &todo) {
     constexpr int N = (D + 63) / 64, V = 16 / (int)sizeof(S);
