@@ -225,9 +225,10 @@ template <typename S, int D> struct Tile {
 
     // Rows [0, N) at `src`, `stride` bytes apart (64 of them below 2^31 bytes), to `dst` by the
     // buffer loads that write LDS directly.  Rows from `valid` (>= 1) on are read past the
-    // buffer's end and come back as zeros: a weight of 0 never meets an infinity there.  The
-    // loads are shared by NW waves; this is wave w.
-    template <int N, int NW>
+    // buffer's end and come back as zeros: a weight of 0 never meets an infinity there.  LAST: they
+    // repeat the last valid row, which has no product that this one has not (a zero has: with
+    // an infinity, a NaN).  The loads are shared by NW waves; this is wave w.
+    template <int N, int NW, bool LAST = false>
     __device__ __forceinline__ static void stage(char *dst, const char *src, long long stride, int valid, int w) {
         constexpr int loads = N / kRowsPerLoad, each = (loads + NW - 1) / NW;
         const int lane = threadIdx.x & 63;
@@ -239,7 +240,7 @@ template <typename S, int D> struct Tile {
 #pragma unroll
         for (int a = 0; a < each; ++a) {
             const int r = (a * NW + w) * kRowsPerLoad + rr;
-            off[a] = r < valid ? r * st + 16 * (pc ^ swz(r)) : 0x7fffff00;
+            off[a] = r < valid || LAST ? min(r, valid - 1) * st + 16 * (pc ^ swz(r)) : 0x7fffff00;
         }
         if constexpr (each % 4 == 0) {
 #pragma unroll
@@ -325,6 +326,24 @@ __device__ __forceinline__ float dot_rows(const float *a, const float *b, int ks
     for (int j = 0; j < 8; ++j) s = fmaf(a[16 * ks + 8 * h + j], b[16 * ks + 8 * h + j], s);
     return s;
 }
+
+// The inner product of two rows, by one lane.
+template <typename S, int D> __device__ __forceinline__ float dot_row(const S *a, const S *b) {
+    constexpr int V = 16 / (int)sizeof(S);
+    float s = 0.f;
+    for (int d = 0; d < D; d += V) {
+        float x[V], y[V];
+        Vec<S>::load(a + d, x);
+        Vec<S>::load(b + d, y);
+#pragma unroll
+        for (int e = 0; e < V; ++e) s = fmaf(x[e], y[e], s);
+    }
+    return s;
+}
+__device__ __forceinline__ float value_of(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ float value_of(float x) { return x; }
+__device__ __forceinline__ void put_value(uint16_t *p, float x) { *p = (uint16_t)f32_to_bf16(x); }
+__device__ __forceinline__ void put_value(float *p, float x) { *p = x; }
 
 // Stores the lane's column of D / 32 results (column = a row of the output, rows = its
 // values) times `scale`.  Both halves of a row must be active.

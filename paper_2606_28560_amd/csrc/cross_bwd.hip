@@ -214,16 +214,75 @@ template <typename S, int D> struct DqItem {
                 }
         }
     }
-    // Columns 32 dt .. of the lane's row of dq, or of its piece.
-    template <int N> __device__ __forceinline__ void store(const Gradients &a, int d, const f32x16_t *acc) const {
+    // Columns 32 dt .. of the lane's row of dq, or of its piece, unless it is one of `skip`.
+    template <int N>
+    __device__ __forceinline__ void store(const Gradients &a, int d, const f32x16_t *acc, uint32_t skip) const {
         const int h = (threadIdx.x >> 5) & 1;
-        if (!on) return;
+        if (!on || (skip >> (threadIdx.x & 31) & 1)) return;
         if (a.dq_pieces > 1)
             store_cols<N>(a.dq_part + (piece * ((long long)a.B * a.H * a.T) + id) * D + d, acc, a.tau, h);
         else
             store_cols<N>((S *)a.dq + b * a.ldq.sb + hh * a.ldq.sh + t * a.ldq.st + d, acc, a.tau, h);
     }
 };
+
+// Rows of `which` (bit i: the row of lane i) of an item of dq, by the whole wave: a lane to each
+// of 64 rows of the states [c0, c1) for the weights, a lane to each value for the sum.
+//
+// An infinity in a row of the states makes NaN of its float32 products (the parts of a value), of
+// the row's weight and so of every value of dq.  Here a weight of 0 is 0, and what is not finite
+// stays where the formula has it, in the elements that are infinite themselves.
+template <typename S, int D>
+__device__ __forceinline__ void plain_dq(const Gradients &a, const DqItem<S, D> &x, const DqRows<S, D> &w, uint32_t which,
+                                         int c0, int c1) {
+    constexpr int N = (D + 63) / 64;
+    const int lane = threadIdx.x & 63;
+    const S *k = (const S *)x.kp, *v = (const S *)x.vp;
+    for (; which; which &= which - 1) {
+        const int i = __builtin_ctz(which);
+        const int b = __shfl(x.b, i, 64), hh = __shfl(x.hh, i, 64), t = __shfl(x.t, i, 64);
+        const float lse2 = __shfl(w.lse2, i, 64), delta = __shfl(w.delta, i, 64);
+        const S *q = (const S *)a.q + b * a.lq.sb + hh * a.lq.sh + t * a.lq.st;
+        const S *g = (const S *)a.g + b * a.lg.sb + hh * a.lg.sh + t * a.lg.st;
+        float y[N];
+#pragma unroll
+        for (int n = 0; n < N; ++n) y[n] = 0.f;
+        for (int c = c0; c < c1; c += 64) {
+            float ds = 0.f;
+            if (c + lane < c1) {
+                const float s = dot_row<S, D>(q, k + (c + lane) * a.lk.st);
+                ds = ex2(fmaf(s, a.scale, -lse2)) * (dot_row<S, D>(g, v + (c + lane) * a.lv.st) + delta);
+            }
+            const int count = min(64, c1 - c);
+            for (int e = 0; e < count; ++e) {
+                const float d = __shfl(ds, e, 64);
+#pragma unroll
+                for (int n = 0; n < N; ++n)
+                    if (lane + 64 * n < D) y[n] = fmaf(d, value_of(k[(c + e) * a.lk.st + lane + 64 * n]), y[n]);
+            }
+        }
+        const long long id = ((long long)b * a.H + hh) * a.T + t;
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            if (lane + 64 * n < D) {
+                if (a.dq_pieces > 1)
+                    a.dq_part[(x.piece * ((long long)a.B * a.H * a.T) + id) * D + lane + 64 * n] = y[n] * a.tau;
+                else
+                    put_value((S *)a.dq + b * a.ldq.sb + hh * a.ldq.sh + t * a.ldq.st + lane + 64 * n, y[n] * a.tau);
+            }
+    }
+}
+
+// Rows that plain_dq does (bit i: the row of lane i), from any value of the lane's row: float32
+// rows that are not a number though their lse and D are finite (a weight that is none makes all
+// of a row so).
+template <typename S, int D>
+__device__ __forceinline__ uint32_t odd_rows(const DqItem<S, D> &x, const DqRows<S, D> &w, float any) {
+    if constexpr (sizeof(S) == 2) return 0;
+    const unsigned long long bad =
+        __ballot(x.on && any != any && fabsf(w.lse2) < INFINITY && fabsf(w.delta) < INFINITY);
+    return (uint32_t)(bad | bad >> 32);
+}
 
 // 128 query rows a workgroup, 32 to a wave; the rows of the states are staged for all four.
 template <typename S, int D>
@@ -272,7 +331,9 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
         step(i, 0);
         if (i + 1 < n1) step(i + 1, 1);
     }
-    x.template store<D>(a, 0, w.acc);
+    const uint32_t odd = odd_rows<S, D>(x, w, w.acc[0][0]);
+    x.template store<D>(a, 0, w.acc, odd);
+    if (odd) plain_dq<S, D>(a, x, w, odd, n0 * NT, min(n1 * NT, len));
 }
 
 // The four waves' results of the same columns, added in the order of the waves: wave w hands
@@ -301,6 +362,11 @@ __device__ __forceinline__ void add_waves(const f32x16_t *acc, char *lds, int wv
             }
         put(dt, sum);
     }
+}
+
+// Every N-th of 32 bits, from bit wv on (N 1, 2 or 4).
+template <int N> __device__ __forceinline__ uint32_t every(int wv) {
+    return (N == 1 ? 0xffffffffu : N == 2 ? 0x55555555u : 0x11111111u) << wv;
 }
 
 // Stages of a wave's own: two where a tile's products are shorter than its way from memory
@@ -358,7 +424,13 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dq_narrow_kernel(
             fetch_k(i + 4, kt);
         }
     }
-    add_waves<N>(w.acc, lds, wv, [&](int dt, const f32x16_t &sum) { x.template store<32>(a, 32 * dt, &sum); });
+    uint32_t odd = 0;  // known to the first N waves, which do every N-th of them
+    add_waves<N>(w.acc, lds, wv, [&](int dt, const f32x16_t &sum) {
+        odd = odd_rows<S, D>(x, w, sum[0]);
+        x.template store<32>(a, 32 * dt, &sum, odd);
+    });
+    odd &= every<N>(wv);
+    if (odd) plain_dq<S, D>(a, x, w, odd, 32 * n0, min(32 * n1, len));
 }
 
 // One item of the dk, dv kernels: its problem, its piece of the queries, the lane's row of the
@@ -377,10 +449,12 @@ template <typename S, int D> struct KvItem {
         n0 = (int)((long long)n * piece / a.dkv_pieces);
         n1 = (int)((long long)n * (piece + 1) / a.dkv_pieces);
     }
+    __device__ __forceinline__ const S *row(const Gradients &a, const void *p, const Layout &l, int cc) const {
+        return (const S *)p + b0 * l.sb + j * l.sh + cc * l.st;
+    }
     __device__ __forceinline__ void load(const Gradients &a, KvRows<typename KvValue<S, D>::type, D> &w) const {
         const int h = (threadIdx.x >> 5) & 1, cc = min(c, len - 1);
-        const S *k = (const S *)a.k + b0 * a.lk.sb + j * a.lk.sh + cc * a.lk.st;
-        const S *v = (const S *)a.v + b0 * a.lv.sb + j * a.lv.sh + cc * a.lv.st;
+        const S *k = row(a, a.k, a.lk, cc), *v = row(a, a.v, a.lv, cc);
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks) {
             load_frag(k, ks, h, w.k[ks]);
@@ -410,23 +484,25 @@ template <typename S, int D> struct KvItem {
     template <int NW> __device__ __forceinline__ void fetch_g(const Gradients &a, const At &at, char *dst, int w) const {
         typedef Tile<S, D> X;
         const S *g = (const S *)a.g + (b0 + at.bb) * a.lg.sb + (j * a.G + at.g) * a.lg.sh + 32 * at.tt * a.lg.st;
-        X::template stage<32, NW>(dst + X::bytes(32), (const char *)g, a.lg.st * (long long)sizeof(S), a.T - 32 * at.tt, w);
+        X::template stage<32, NW, true>(dst + X::bytes(32), (const char *)g, a.lg.st * (long long)sizeof(S), a.T - 32 * at.tt, w);
     }
     template <int NW> __device__ __forceinline__ void fetch_q(const Gradients &a, const At &at, char *dst, int w) const {
         typedef Tile<S, D> X;
         const int b = b0 + at.bb, hh = j * a.G + at.g;
         const S *q = (const S *)a.q + b * a.lq.sb + hh * a.lq.sh + 32 * at.tt * a.lq.st;
-        X::template stage<32, NW>(dst, (const char *)q, a.lq.st * (long long)sizeof(S), a.T - 32 * at.tt, w);
+        X::template stage<32, NW, true>(dst, (const char *)q, a.lq.st * (long long)sizeof(S), a.T - 32 * at.tt, w);
         if (w == NW - 1)
             load_lds4(uniform(lds_address(dst + 2 * X::bytes(32))),
                       buffer_of(a.stats + (((long long)b * a.H + hh) * tiles + at.tt) * 64, 256),
                       4 * (int)(threadIdx.x & 63));
     }
-    // Columns d .. d + N - 1 of the lane's row of dk (which 0) or dv (1), or of its piece.
+    // Columns d .. d + N - 1 of the lane's row of dk (which 0) or dv (1), or of its piece, unless it
+    // is one of `skip`.
     template <int N>
-    __device__ __forceinline__ void store(const Gradients &a, int which, int d, const f32x16_t *acc, float scale) const {
+    __device__ __forceinline__ void store(const Gradients &a, int which, int d, const f32x16_t *acc, float scale,
+                                          uint32_t skip) const {
         const int h = (threadIdx.x >> 5) & 1;
-        if (c >= a.S) return;
+        if (c >= a.S || (skip >> (threadIdx.x & 31) & 1)) return;
         const f32x16_t none[N / 32] = {};
         const f32x16_t *x = c < len ? acc : none;  // 0 for rows that no query reads
         if (a.dkv_pieces > 1) {
@@ -435,6 +511,70 @@ template <typename S, int D> struct KvItem {
         } else {
             const Layout &l = which ? a.ldv : a.ldk;
             store_cols<N>((S *)(which ? a.dv : a.dk) + b0 * l.sb + j * l.sh + c * l.st + d, x, scale, h);
+        }
+    }
+    // Rows that plain() does (bit i: the row of lane i), from any value of the lane's row of dk or dv:
+    // those that are not a number and whose key holds an infinity (in bfloat16's range) but no NaN.
+    // An infinity has no parts: where a product takes them its logits are NaN, and all of dk and dv,
+    // though they may be -inf and their weights 0.
+    __device__ __forceinline__ uint32_t odd(const Gradients &a, float any) const {
+        if constexpr (sizeof(S) == 2 || D == 128) return 0;  // (float32 d 128 multiplies whole values)
+        if (!__ballot(c < len && any != any)) return 0;
+        const S *k = row(a, a.k, a.lk, min(c, len - 1));
+        float top = 0.f, sum = 0.f;
+        for (int d = 0; d < D; ++d) {
+            const float x = fabsf(value_of(k[d]));
+            top = fmaxf(top, x);
+            sum += x;
+        }
+        return (uint32_t)__ballot(c < len && any != any && top >= 0x1.ffp127f && sum == sum);
+    }
+    // The rows of `which`, each by the whole wave: a lane to each of a tile's queries for the weights,
+    // a lane to each value for the sums.
+    __device__ __forceinline__ void plain(const Gradients &a, uint32_t which) const {
+        constexpr int N = (D + 63) / 64;
+        const int lane = threadIdx.x & 63, row0 = __builtin_amdgcn_readfirstlane(c);
+        for (; which; which &= which - 1) {
+            const int cc = row0 + __builtin_ctz(which);
+            const S *k = row(a, a.k, a.lk, cc), *v = row(a, a.v, a.lv, cc);
+            float dk[N], dv[N];
+#pragma unroll
+            for (int n = 0; n < N; ++n) dk[n] = dv[n] = 0.f;
+            auto at = tile_at(a, n0);
+            for (int i = n0; i < n1; ++i) {
+                const int b = b0 + at.bb, hh = j * a.G + at.g, count = min(32, a.T - 32 * at.tt);
+                const S *q = (const S *)a.q + b * a.lq.sb + hh * a.lq.sh + 32 * at.tt * a.lq.st;
+                const S *g = (const S *)a.g + b * a.lg.sb + hh * a.lg.sh + 32 * at.tt * a.lg.st;
+                const float *st = a.stats + (((long long)b * a.H + hh) * tiles + at.tt) * 64;
+                float p = 0.f, ds = 0.f;
+                if (lane < count) {
+                    p = ex2(fmaf(dot_row<S, D>(q + lane * a.lq.st, k), a.scale, -st[lane]));
+                    ds = p * (dot_row<S, D>(g + lane * a.lg.st, v) + st[32 + lane]);
+                }
+                for (int e = 0; e < count; ++e) {
+                    const float pe = __shfl(p, e, 64), de = __shfl(ds, e, 64);
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+                        if (lane + 64 * n < D) {
+                            dk[n] = fmaf(de, value_of(q[e * a.lq.st + lane + 64 * n]), dk[n]);
+                            dv[n] = fmaf(pe, value_of(g[e * a.lg.st + lane + 64 * n]), dv[n]);
+                        }
+                }
+                step(a, at, 1);
+            }
+            const long long part = (piece * ((long long)a.Bkv * a.Hkv * a.S) + (long long)prob * a.S + cc) * D;
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+                if (lane + 64 * n < D) {
+                    const int d = lane + 64 * n;
+                    if (a.dkv_pieces > 1) {
+                        a.dk_part[part + d] = dk[n] * a.tau;
+                        a.dv_part[part + d] = dv[n];
+                    } else {
+                        put_value((S *)a.dk + b0 * a.ldk.sb + j * a.ldk.sh + cc * a.ldk.st + d, dk[n] * a.tau);
+                        put_value((S *)a.dv + b0 * a.ldv.sb + j * a.ldv.sh + cc * a.ldv.st + d, dv[n]);
+                    }
+                }
         }
     }
 };
@@ -483,14 +623,18 @@ __global__ __launch_bounds__(256, sizeof(S) == 4 && D == 128 ? 1 : 2) void cross
             if (i + 1 < x.n1) step(i + 1, 1);
         }
     }
-    x.template store<D>(a, 0, 0, w.dk, a.tau);
-    x.template store<D>(a, 1, 0, w.dv, 1.f);
+    const uint32_t odd = x.odd(a, w.dk[0][0]);
+    x.template store<D>(a, 0, 0, w.dk, a.tau, odd);
+    x.template store<D>(a, 1, 0, w.dv, 1.f, odd);
+    if (odd) x.plain(a, odd);
 }
 
 // 32 rows of the states for all four waves, each on its own tiles of queries, staged for the
-// wave alone: for problems too few to fill the CUs by 128 rows.
+// wave alone: for problems too few to fill the CUs by 128 rows.  (d 32: the registers of float32
+// held down for a third wave to a SIMD, 161 for 169: 46.1 for 47.7 microseconds at 4 x 8 heads of
+// 700 x 900.)
 template <typename S, int D>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dkdv_narrow_kernel(Gradients a, int items) {
+__global__ __launch_bounds__(256, D == 128 ? 1 : D == 64 ? 2 : 3) void cross_dkdv_narrow_kernel(Gradients a, int items) {
     typedef Tile<S, D> X;
     constexpr int NB = kPrivate<S>, N = D / 32, SB = 2 * X::bytes(32) + 256;
     __shared__ __attribute__((aligned(16))) char lds[4 * NB * SB > 16384 * N ? 4 * NB * SB : 16384 * N];
@@ -538,8 +682,14 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void cross_dkdv_narrow_kerne
             }
         }
     }
-    add_waves<N>(w.dk, lds, wv, [&](int dt, const f32x16_t &sum) { x.template store<32>(a, 0, 32 * dt, &sum, a.tau); });
-    add_waves<N>(w.dv, lds, wv, [&](int dt, const f32x16_t &sum) { x.template store<32>(a, 1, 32 * dt, &sum, 1.f); });
+    uint32_t odd = 0;  // as in dq
+    add_waves<N>(w.dk, lds, wv, [&](int dt, const f32x16_t &sum) {
+        odd = x.odd(a, sum[0]);
+        x.template store<32>(a, 0, 32 * dt, &sum, a.tau, odd);
+    });
+    add_waves<N>(w.dv, lds, wv, [&](int dt, const f32x16_t &sum) { x.template store<32>(a, 1, 32 * dt, &sum, 1.f, odd); });
+    odd &= every<N>(wv);
+    if (odd) x.plain(a, odd);
 }
 
 // Sums the pieces of up to three gradients, in the order of the pieces.

@@ -357,11 +357,6 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
     if (which) todo = {which, b0, j, 32 * tile, 32 * n0, min(32 * n1, len), len, slot};
 }
 
-__device__ __forceinline__ float value_of(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-__device__ __forceinline__ float value_of(float x) { return x; }
-__device__ __forceinline__ void put_value(uint16_t *p, float x) { *p = (uint16_t)f32_to_bf16(x); }
-__device__ __forceinline__ void put_value(float *p, float x) { *p = x; }
-
 // The rows of `todo`, each by the whole wave: a lane to each of 64 rows of the states, and only
 // to those that the query reads, for the weights; a lane to each value for the sums.
 //
@@ -371,7 +366,7 @@ __device__ __forceinline__ void put_value(float *p, float x) { *p = x; }
 // largest one is subtracted from it, whose weight then is 1.
 template <typename S, int D>
 __device__ __forceinline__ void plain_rows(const Queries &a, const States &st, const Redo &todo) {
-    constexpr int N = (D + 63) / 64, V = 16 / (int)sizeof(S);
+    constexpr int N = (D + 63) / 64;
     const int lane = threadIdx.x & 63;
     const S *k = (const S *)st.k + todo.b0 * st.lk.sb + todo.j * st.lk.sh;
     const S *v = (const S *)st.v + todo.b0 * st.lv.sb + todo.j * st.lv.sh;
@@ -385,17 +380,7 @@ __device__ __forceinline__ void plain_rows(const Queries &a, const States &st, c
         for (int n = 0; n < N; ++n) y[n] = 0.f;
         for (int c = todo.c0; c < lim; c += 64) {
             float s = -INFINITY;
-            if (c + lane < lim) {
-                s = 0.f;
-                for (int d = 0; d < D; d += V) {
-                    float x[V], z[V];
-                    Vec<S>::load(q + d, x);
-                    Vec<S>::load(k + (c + lane) * st.lk.st + d, z);
-#pragma unroll
-                    for (int e = 0; e < V; ++e) s = fmaf(x[e], z[e], s);
-                }
-                s *= a.scale;
-            }
+            if (c + lane < lim) s = dot_row<S, D>(q, k + (c + lane) * st.lk.st) * a.scale;
             // a NaN stays one: fmaxf drops it, its weight below does not
             float top = s;
 #pragma unroll
