@@ -170,18 +170,19 @@ __device__ __forceinline__ uint32_t uniform(uint64_t x) {
 // zeros do.  Written in assembly, without a register loaded, so that reads of other LDS do not
 // wait for them: their own readers do so by wait_loads and, across waves, a barrier.  s_nop 4:
 // the wait states between a vector write of a scalar register (a spilled one restored, say) and
-// its use by a load; s_nop 0: between m0 and a load to LDS.
+// its use by a load; s_nop 0: between m0 and a load to LDS.  m0 is named to the compiler as
+// written: it keeps nothing there across them.
 __device__ __forceinline__ void load_lds4(uint32_t to, u32x4_t buf, int off) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
                  :
                  : "s"(to), "v"(off), "s"(buf)
-                 : "memory");
+                 : "memory", "m0");
 }
 __device__ __forceinline__ void load_lds16(uint32_t to, u32x4_t buf, int off) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
                  :
                  : "s"(to), "v"(off), "s"(buf)
-                 : "memory");
+                 : "memory", "m0");
 }
 // Four of them, `step` bytes of LDS apart.
 __device__ __forceinline__ void load_lds16(uint32_t to, uint32_t step, u32x4_t buf, const int *off) {
@@ -191,7 +192,7 @@ __device__ __forceinline__ void load_lds16(uint32_t to, uint32_t step, u32x4_t b
                  "s_add_u32 m0, m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %5, %6, 0 offen lds"
                  :
                  : "s"(to), "s"(step), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(buf)
-                 : "memory", "scc");
+                 : "memory", "m0", "scc");
 }
 __device__ __forceinline__ u32x4_t buffer_of(const void *src, uint32_t bytes) {
     const uint64_t base = (uint64_t)src;
