@@ -170,8 +170,11 @@ __device__ __forceinline__ uint32_t uniform(uint64_t x) {
 // zeros do.  Written in assembly, without a register loaded, so that reads of other LDS do not
 // wait for them: their own readers do so by wait_loads and, across waves, a barrier.  s_nop 4:
 // the wait states between a vector write of a scalar register (a spilled one restored, say) and
-// its use by a load; s_nop 0: between m0 and a load to LDS.  m0 is named to the compiler as
-// written: it keeps nothing there across them.
+// its use by a load; s_nop 0: between m0 and a load to LDS.  m0 is named as written, so that no
+// setting of it is kept across them (that it is a register the compiler reserves is what it
+// would warn of).
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_lds4(uint32_t to, u32x4_t buf, int off) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dword %1, %2, 0 offen lds"
                  :
@@ -194,6 +197,7 @@ __device__ __forceinline__ void load_lds16(uint32_t to, uint32_t step, u32x4_t b
                  : "s"(to), "s"(step), "v"(off[0]), "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"(buf)
                  : "memory", "m0", "scc");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ u32x4_t buffer_of(const void *src, uint32_t bytes) {
     const uint64_t base = (uint64_t)src;
     return u32x4_t{uniform(base), uniform((base >> 32) & 0xffffu), uniform(bytes), 0x00027000u};
