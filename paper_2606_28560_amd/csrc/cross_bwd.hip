@@ -767,14 +767,13 @@ double tile_us(int dtype, int D, bool dkv) {
 }
 
 // How a gradient over `rows` rows to a problem is computed: narrow workgroups (32 rows, the
-// other side's rows divided among the waves) or wide ones (128 rows), and in how many pieces
-// of the other side's `steps` rows: the least of an estimate of the time.  Wide and narrow dk,
+// other side's tiles divided among the waves) or wide ones (128 rows), and in how many pieces
+// of the other side's n tiles: the least of an estimate of the time.  Wide and narrow dk,
 // dv measured, in their best pieces, without the pieces' sum: 117 and 201 microseconds at 2 x 16
 // heads on 4 of 1000 x 2500, d 128, bfloat16; 32 (two or more pieces) and 30 (one) at 4 x 8 heads
 // of 200 x 200, d 128, float32.
-void divide(int dtype, int D, long long prob, int rows, int steps, bool dkv, int *narrow, int *tiles, int *pieces) {
+void divide(int dtype, int D, long long prob, int rows, int n, bool dkv, int *narrow, int *tiles, int *pieces) {
     const double us = tile_us(dtype, D, dkv);
-    const int n = (steps + 31) / 32;
     double best = 1e30;
     for (int wide = 0; wide < 2; ++wide) {
         const int t = (rows + (wide ? 127 : 31)) / (wide ? 128 : 32);
@@ -800,8 +799,10 @@ void divide(int dtype, int D, long long prob, int rows, int steps, bool dkv, int
 
 void plan_cross_backward(int dtype, int D, Gradients *a) {
     const long long prob = (long long)a->Bkv * a->Hkv;
-    divide(dtype, D, prob, a->rows, a->S, false, &a->dq_narrow, &a->row_tiles, &a->dq_pieces);
-    divide(dtype, D, prob, a->S, a->rows, true, &a->dkv_narrow, &a->key_tiles, &a->dkv_pieces);
+    divide(dtype, D, prob, a->rows, (a->S + 31) / 32, false, &a->dq_narrow, &a->row_tiles, &a->dq_pieces);
+    // a tile of queries is of one head and one batch entry, however few positions it has
+    divide(dtype, D, prob, a->S, (a->T + 31) / 32 * a->G * a->share, true, &a->dkv_narrow, &a->key_tiles,
+           &a->dkv_pieces);
 }
 
 hipError_t launch_cross_backward(int dtype, int D, const Gradients &a, hipStream_t s) {
