@@ -13,7 +13,7 @@
 // bfloat16 steps take 192 cycles of a matrix core where v_mfma_f32_32x32x2_f32 takes 512
 // (with the parts' making, forward and dq 1.2 to 1.35 times as fast, dk and dv 1.1 to 1.2 at
 // d 64 and 32).  The parts of d 128's rows of k and v are too many registers beside dk and dv:
-// those kernels take the float32 instructions (whole_t; 30 against 40 microseconds at 4 x 8
+// those kernels take the float32 instructions (whole_t; 29 against 40 microseconds at 4 x 8
 // heads of 200 x 200).
 //
 // The kernels form the transposed logits, so that a lane holds one query's (dk, dv: one

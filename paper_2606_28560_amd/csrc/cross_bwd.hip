@@ -3,6 +3,10 @@
 //   p_rj = exp(s_rj - lse_r),  D_r = <dO_r, o_r>,  dS_rj = p_rj (<dO_r, v_j> - D_r),
 //   dq_r = tau sum_j dS_rj k_j,  dk_j = tau sum_r dS_rj q_r,  dv_j = sum_r p_rj dO_r,
 //
+// D from the o that was stored, whose rounding it has (2^-8 of its terms in bfloat16): its other
+// form, sum_j p_rj <dO_r, v_j>, holds only where these states are the whole softmax, and needs
+// a pass over them before dq's.  Of lse_r and o_r those of a softmax over more keys do as well.
+//
 // the sums over r running over every query head (and, for states that the batch shares,
 // every batch entry) that reads the key/value head.  The weights are formed again in each
 // kernel: dq goes by rows and passes over the states, dk and dv go by the states' rows and

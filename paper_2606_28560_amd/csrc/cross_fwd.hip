@@ -506,7 +506,8 @@ __global__ __launch_bounds__(256) void join_parts_kernel(Queries a, int parts) {
         *reinterpret_cast<uint2 *>(row) = make_uint2(pack2(y[0] * f, y[1] * f), pack2(y[2] * f, y[3] * f));
 }
 
-// The same for two stored results over disjoint sets of keys.
+// The same for two stored results over disjoint sets of keys, whose rounding to the storage type
+// (2^-8 of each in bfloat16) they bring with them; partial results of one call are float32.
 template <typename S, int D>
 __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
     constexpr int N = 16 / (int)sizeof(S), per = D / N;
