@@ -263,7 +263,7 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
     typedef Tile<S, D> X;
     constexpr int TB = X::bytes(32), OPS = 32 / X::kRowsPerLoad;
     __shared__ float stat[2][4][32];
-    __shared__ uint32_t odd_rows;
+    __shared__ uint32_t odd_rows[32];
     const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5;
     const int tile = item % st.tiles, piece = item / st.tiles % st.splits, prob = item / st.tiles / st.splits;
     const int b0 = prob / a.Hkv, j = prob % a.Hkv;
@@ -307,7 +307,7 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
         stat[0][wv][lane] = w.m;
         stat[1][wv][lane] = l;
     }
-    if (threadIdx.x == 0) odd_rows = 0;
+    if (threadIdx.x < 32) odd_rows[threadIdx.x] = 0;
     __syncthreads();
     constexpr int V = 4, per = D / V, each = 32 * per / 256;  // lanes to a row, values of a lane
     f32x4_t y[each];
@@ -327,13 +327,13 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
             sum += stat[1][x][r] * f;
             y[e] += *reinterpret_cast<const f32x4_t *>(part + (32 * x + r) * D + d) * f;
         }
-        if (again<S>((y[e][0] + y[e][1]) * 0.f + (y[e][2] + y[e][3]) * 0.f, sum, m)) atomicOr(&odd_rows, 1u << r);
+        if (again<S>((y[e][0] + y[e][1]) * 0.f + (y[e][2] + y[e][3]) * 0.f, sum, m)) odd_rows[r] = 1;
         y[e] *= sum == 0.f ? 0.f : 1.f / sum;
         lse[e] = sum == 0.f ? -INFINITY : (m + __log2f(sum)) * kLn2;
     }
     __syncthreads();
     const long long slot = st.slot + piece;
-    const uint32_t odd = odd_rows;
+    const uint32_t odd = (uint32_t)__ballot(odd_rows[lane & 31] != 0);
 #pragma unroll
     for (int e = 0; e < each; ++e) {
         const int r = (threadIdx.x + 256 * e) / per, d = (threadIdx.x + 256 * e) % per * V;
