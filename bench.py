@@ -63,15 +63,15 @@ def parse_args():
 #            --no-learned-alpha --no-integer-offsets --no-rope-on-load --no-configs --copy-probe-mb 256
 # each scaled by what the same counter reads for the plain 256 MiB device copy of that run.
 # They hold only for the kernel sources they were taken on (COUNTER_SOURCES_SHA).
-COUNTER_SOURCES_SHA = "14cbc1225a18006af4b21ef2f80149cd162428c430902f6a5e3bd408d4172c34"
+COUNTER_SOURCES_SHA = "d69b1b528fb69e9b283f4c170f68f624d20567dc94ea904363cb31552f5961e6"
 COUNTER_WORKLOAD = "layer_60m_fixed_T1024"
 COUNTER_KIB = {  # kernel: (FETCH_SIZE, WRITE_SIZE) mean KiB per dispatch
-    "forward": (12407.9, 16754.9),
-    "bwd_dq": (20801.1, 10426.1),
-    "bwd_dkdv": (18578.5, 16595.1),
-    "rope": (4128.9, 8192.0),
+    "forward": (12407.9, 16753.1),
+    "bwd_dq": (20789.1, 10425.9),
+    "bwd_dkdv": (18554.3, 16606.1),
+    "rope": (4128.8, 8192.0),
 }
-COPY_PROBE_KIB = (262144.0, 131091.8, 262144.0)  # bytes moved each way; FETCH_SIZE; WRITE_SIZE
+COPY_PROBE_KIB = (262144.0, 131092.6, 262144.0)  # bytes moved each way; FETCH_SIZE; WRITE_SIZE
 
 
 def kernel_sources_sha() -> str:
