@@ -357,13 +357,21 @@ __device__ __forceinline__ void keys_body(const Queries &a, const States &st, in
     if (which) todo = {which, b0, j, 32 * tile, 32 * n0, min(32 * n1, len), len, slot};
 }
 
+// x y, rounded whatever is done with it next.
+__device__ __forceinline__ float rounded(float x, float y) {
+#pragma clang fp contract(off)
+    return x * y;
+}
+
 // The rows of `todo`, each by the whole wave: a lane to each of 64 rows of the states, and only
 // to those that the query reads, for the weights; a lane to each value for the sums.
 //
 // The tiles multiply what a query does not read by a weight of 0, and the rest of a weight may
 // be 0 or negative: with an infinity or NaN among the values either makes a NaN of what is not
 // one.  Here nothing unread enters, every weight is whole, and a logit is rounded before the
-// largest one is subtracted from it, whose weight then is 1.
+// largest one is subtracted from it, whose weight then is 1.  There are at most 2^30 weights of at
+// most 1: 2^-31 of them, and the 2^31 with the division by their sum, keep the sums of large values
+// from overflowing as the tiles' may (bits are lost of products below 2^-94).
 template <typename S, int D>
 __device__ __forceinline__ void plain_rows(const Queries &a, const States &st, const Redo &todo) {
     constexpr int N = (D + 63) / 64;
@@ -380,7 +388,7 @@ __device__ __forceinline__ void plain_rows(const Queries &a, const States &st, c
         for (int n = 0; n < N; ++n) y[n] = 0.f;
         for (int c = todo.c0; c < lim; c += 64) {
             float s = -INFINITY;
-            if (c + lane < lim) s = dot_row<S, D>(q, k + (c + lane) * st.lk.st) * a.scale;
+            if (c + lane < lim) s = rounded(dot_row<S, D>(q, k + (c + lane) * st.lk.st), a.scale);
             // a NaN stays one: fmaxf drops it, its weight below does not
             float top = s;
 #pragma unroll
@@ -397,13 +405,13 @@ __device__ __forceinline__ void plain_rows(const Queries &a, const States &st, c
             for (int n = 0; n < N; ++n) y[n] *= f;
             const int count = min(64, lim - c);
             for (int e = 0; e < count; ++e) {
-                const float w = __shfl(p, e, 64);
+                const float w = __shfl(p, e, 64) * 0x1p-31f;
 #pragma unroll
                 for (int n = 0; n < N; ++n)
                     if (lane + 64 * n < D) y[n] = fmaf(w, value_of(v[(c + e) * st.lv.st + lane + 64 * n]), y[n]);
             }
         }
-        const float f = l == 0.f ? 0.f : 1.f / l;
+        const float f = l == 0.f ? 0.f : 0x1p31f / l;
         if (lane == 0) put_lse(a, todo.slot, id, m, l);
 #pragma unroll
         for (int n = 0; n < N; ++n)
@@ -454,7 +462,8 @@ __global__ __launch_bounds__(RW ? 512 : 256, (simd_waves<S, D, RW>())) void cros
 
 // Partial results of a row: o = sum_i exp(lse_i - lse) o_i, lse = log sum_i exp(lse_i).  A
 // part without rows (lse -inf) counts nothing, whatever its o holds.  A wave to a row: lane i
-// has the weight of part i (at most 64 at a time), and D / 4 lanes add every (256 / D)-th part.
+// has the weights of parts i and 64 + i (there are at most 128), of sum 1, so that no sum of
+// values overflows; D / 4 lanes add every (256 / D)-th part.
 template <typename S, int D>
 __global__ __launch_bounds__(256) void join_parts_kernel(Queries a, int parts) {
     constexpr int per = D / 4, groups = 64 / per;
@@ -462,18 +471,24 @@ __global__ __launch_bounds__(256) void join_parts_kernel(Queries a, int parts) {
     const long long r = ((long long)blockIdx.y * gridDim.x + blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (r >= rows) return;
     const int lane = threadIdx.x & 63, g = lane / per, d = lane % per * 4;
-    float m = -INFINITY;
-    for (int i = lane; i < parts; i += 64) m = fmaxf(m, a.part_lse[i * rows + r]);
+    float z[2], f[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) z[c] = lane + 64 * c < parts ? a.part_lse[(lane + 64 * c) * rows + r] : -INFINITY;
+    float m = fmaxf(z[0], z[1]);
 #pragma unroll
     for (int e = 32; e; e >>= 1) m = fmaxf(m, __shfl_xor(m, e, 64));
-    float sum = 0.f;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) f[c] = z[c] == -INFINITY ? 0.f : ex2((z[c] - m) * kLog2e);
+    float sum = f[0] + f[1];
+#pragma unroll
+    for (int e = 32; e; e >>= 1) sum += __shfl_xor(sum, e, 64);
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
     f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-    for (int base = 0; base < parts; base += 64) {
-        const int n = min(64, parts - base);
-        const float z = lane < n ? a.part_lse[(base + lane) * rows + r] : -INFINITY;
-        const float f = z == -INFINITY ? 0.f : ex2((z - m) * kLog2e);
-        sum += f;
-        const float *x = a.part_o + ((long long)base * rows + r) * D + d;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const int n = min(64, parts - 64 * c);
+        f[c] *= inv;
+        const float *x = a.part_o + ((long long)(64 * c) * rows + r) * D + d;
         for (int first = 0; first < n; first += 4 * groups) {
             f32x4_t v[4];  // four parts on their way at a time
 #pragma unroll
@@ -484,26 +499,23 @@ __global__ __launch_bounds__(256) void join_parts_kernel(Queries a, int parts) {
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const float w = __shfl(f, min(first + u * groups + g, 63), 64);
+                const float w = __shfl(f[c], min(first + u * groups + g, 63), 64);
                 if (first + u * groups + g < n && w != 0.f) y += v[u] * w;
             }
         }
     }
 #pragma unroll
-    for (int e = 32; e; e >>= 1) sum += __shfl_xor(sum, e, 64);
-#pragma unroll
     for (int e = 32; e >= per; e >>= 1)
 #pragma unroll
         for (int c = 0; c < 4; ++c) y[c] += __shfl_xor(y[c], e, 64);
     if (g) return;
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
     const int t = (int)(r % a.T), h = (int)(r / a.T % a.H), b = (int)(r / a.T / a.H);
     if (d == 0) a.lse[r] = sum == 0.f ? -INFINITY : m + __log2f(sum) * kLn2;
     S *row = out_row<S, D>(a, {b, h, t}) + d;
     if constexpr (sizeof(S) == 4)
-        *reinterpret_cast<f32x4_t *>(row) = y * f;
+        *reinterpret_cast<f32x4_t *>(row) = y;
     else
-        *reinterpret_cast<uint2 *>(row) = make_uint2(pack2(y[0] * f, y[1] * f), pack2(y[2] * f, y[3] * f));
+        *reinterpret_cast<uint2 *>(row) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
 }
 
 // The same for two stored results over disjoint sets of keys, whose rounding to the storage type
