@@ -63,15 +63,15 @@ def parse_args():
 #            --no-learned-alpha --no-integer-offsets --no-rope-on-load --no-configs --copy-probe-mb 256
 # each scaled by what the same counter reads for the plain 256 MiB device copy of that run.
 # They hold only for the kernel sources they were taken on (COUNTER_SOURCES_SHA).
-COUNTER_SOURCES_SHA = "d69b1b528fb69e9b283f4c170f68f624d20567dc94ea904363cb31552f5961e6"
+COUNTER_SOURCES_SHA = "eb58b37f6944357703f776b03381fa0768f2c8078231602d20ff58113df784c4"
 COUNTER_WORKLOAD = "layer_60m_fixed_T1024"
 COUNTER_KIB = {  # kernel: (FETCH_SIZE, WRITE_SIZE) mean KiB per dispatch
-    "forward": (12407.9, 16753.1),
-    "bwd_dq": (20789.1, 10425.9),
-    "bwd_dkdv": (18554.3, 16606.1),
+    "forward": (12407.9, 16751.2),
+    "bwd_dq": (20789.1, 10424.6),
+    "bwd_dkdv": (18562.8, 16614.7),
     "rope": (4128.8, 8192.0),
 }
-COPY_PROBE_KIB = (262144.0, 131092.6, 262144.0)  # bytes moved each way; FETCH_SIZE; WRITE_SIZE
+COPY_PROBE_KIB = (262144.0, 131092.2, 262144.0)  # bytes moved each way; FETCH_SIZE; WRITE_SIZE
 
 
 def kernel_sources_sha() -> str:

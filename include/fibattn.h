@@ -454,9 +454,9 @@ fibattn_status_t fibattn_prefix_forward(const void *q, const void *k_prefix, con
  * The attention over the union of two disjoint sets of keys from the attention over each
  * (of fibattn_forward and fibattn_cross_forward, say): lse = log(exp(lse_a) + exp(lse_b)),
  * o = exp(lse_a - lse) o_a + exp(lse_b - lse) o_b.  A part whose lse is -inf counts nothing
- * whatever its o holds; with both so, o is 0 and lse -inf.  o is rounded once more than its
- * parts, which were when they were stored (bfloat16: up to 2^-8 each; float32 parts, or
- * one call over all keys, have none of it).  o and lse may be o_a and lse_a, or o_b and lse_b.  layouts: o_a, o_b, o, or NULL: packed [B, H, T, d_head].
+ * whatever its o holds; with both so, o is 0 and lse -inf.  o is rounded to dtype where its
+ * parts were rounded already (bfloat16: each by up to 2^-8 of it).  o and lse may be o_a and
+ * lse_a, or o_b and lse_b.  layouts: o_a, o_b, o, or NULL: packed [B, H, T, d_head].
  * Gradients: each part's backward with the joined o and lse gives its own; a sparse layer's
  * dalpha and dtheta come from fibattn_backward_joined alone.
  */
